@@ -53,6 +53,7 @@ extern "C" {
 
 #define F3C_F32 0         /* float32 compute (debug / small models) */
 #define F3C_BF16 1        /* bfloat16 operands, float32 accumulation and residual */
+#define F3C_FP8 2         /* e4m3 rows with power-of-two scales (operators only, not a model dtype) */
 
 #define F3C_MAX_BATCH 64
 #define F3C_STATE_GUIDED 1u   /* state flag: room for guided steps (two passes per sample) */
@@ -386,6 +387,74 @@ int f3c_op_attention(int32_t dtype, int32_t heads, int32_t head_dim, int32_t bat
  * shift/scale f32 [d] or both NULL. d in {128, 256, 512, 1024, 2048}. */
 int f3c_op_ln_mod(int32_t dtype, int32_t rows, int32_t d, const float* h, const float* shift, const float* scale,
                   void* out, f3c_stream stream);
+
+/* 8-bit rows (F3C_FP8): OCP e4m3 values with one scale per block of 128 columns,
+ * a power of two stored as its E8M0 byte (2^(byte - 127)): for activations a
+ * block is 1 x 128 and the scales are bytes [rows][lds], for weights 128 x 128
+ * and [ceil(rows/128)][lds]. Row strides lds of scales are multiples of 4 with
+ * lds >= ceil(K/128), all lds bytes of a row readable (those past the last block
+ * are neither written nor used), scale pointers 4-byte aligned. The last block
+ * of a row, and of rows, may be smaller. */
+
+/* Quantisation of x [rows][ldx] (dtype F3C_F32 or F3C_BF16) to q e4m3 [rows][ldq]
+ * and scale, per block of block_rows x 128 (block_rows 1 or 128). The scale of a
+ * block is the smallest 2^e, e in [-126, 127], with |x| <= 448 * 2^e for all its
+ * finite x (2^-126 if there is none but zeros); q = x * 2^-e, an exact product,
+ * rounded to nearest even. NaN and infinities become NaN and do not count for
+ * the scale. K a multiple of 8; x and q rows 16- and 8-byte aligned. Errors:
+ * F3C_EINVAL (dtype, block_rows, shape, leading dims, NULL or misaligned
+ * pointers). */
+int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K, const void* x, int32_t ldx, void* q,
+                     int32_t ldq, void* scale, int32_t lds, f3c_stream stream);
+
+/* f3c_op_gemm on 8-bit operands: v = A W^T + bias with A e4m3 [M][lda], A_scale
+ * per 1 x 128, W e4m3 [N][ldw], W_scale per 128 x 128, bias f32 [N] or NULL.
+ * epilogue 0: out bf16 [M][ldo] = v; 1: out bf16 = GELU_tanh(v); 2: resid f32
+ * [M][ldr] += (gate ? gate[n] : 1) * v; 3: out e4m3 [M][ldo] and out_scale
+ * [M][ldso] = GELU_tanh(v) quantised per 1 x 128 as f3c_op_quant_fp8 does (from
+ * float32, no rounding in between). Accumulators are float32; the matrix core
+ * adds the products of 8 consecutive k after aligning them to their largest and
+ * drops bits 2^14 below it, so a sum of n normally distributed products is about
+ * 1.3e-5 of its size off. N and K multiples of 16; rows of A, W, out and resid
+ * 16-byte aligned, of bias and gate too; lda and ldw below 2^22. The result of an
+ * output row does not depend on M or on other rows, nor on scheduling. out,
+ * out_scale and resid must not overlap the operands. Errors: F3C_EINVAL. */
+int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,
+                    const void* A_scale, int32_t ldsa, const void* W, int32_t ldw, const void* W_scale, int32_t ldsw,
+                    const float* bias, const float* gate, void* out, int32_t ldo, void* out_scale, int32_t ldso,
+                    float* resid, int32_t ldr, f3c_stream stream);
+
+#define F3C_NORM_NONE 0
+#define F3C_NORM_LAYER 1  /* (x - mean) / sqrt(var + eps), var over the row, biased */
+#define F3C_NORM_RMS 2    /* x / sqrt(mean(x^2) + eps) */
+
+typedef struct {
+  int32_t dtype;          /* of y: F3C_F32 or F3C_BF16 */
+  int32_t out_dtype;      /* F3C_F32, F3C_BF16 or F3C_FP8 */
+  int32_t post;           /* norm of the block's output y */
+  int32_t pre;            /* norm of the updated residual row */
+  float eps;              /* of both norms, > 0 */
+  float resid_scale;
+} f3c_resid_norm_cfg;
+
+/* The pass between two blocks, in one read and write of the rows: for sample b
+ * and its rows off[b]..off[b+1] (B+1 non-decreasing host ints; rows outside are
+ * left alone)
+ *   h   += resid_scale * gate[b] * (post(y) * post_w)
+ *   out  = (pre(h) * pre_w) * (1 + scale[b]) + shift[b]
+ * y [.][ldy] is a block's output, h f32 [.][ldh] the residual, out [.][ldo] the
+ * next block's input (with F3C_FP8: quantised per 1 x 128 from float32, scales in
+ * out_scale [.][lds]). y NULL: h is left as it is (the norm in front of the first
+ * block). out NULL: the update alone. post_w, pre_w f32 [d] or NULL (ones); gate,
+ * shift, scale f32 [B][ldm], ldm = 0 for one row of all samples; gate NULL: ones;
+ * shift and scale both or neither. Statistics are float32, the variance is taken
+ * about the mean. d a multiple of 8, 8..8192; rows and vectors 16-byte aligned
+ * (out rows in F3C_FP8: 8-byte). out, out_scale and h must not overlap other
+ * operands. Errors: F3C_EINVAL. */
+int f3c_op_resid_norm(const f3c_resid_norm_cfg* cfg, int32_t d, int32_t batch, const int32_t* off_host, const void* y,
+                      int32_t ldy, const float* post_w, const float* gate, float* h, int32_t ldh, const float* pre_w,
+                      const float* shift, const float* scale, int32_t ldm, void* out, int32_t ldo, void* out_scale,
+                      int32_t lds, f3c_stream stream);
 
 /* Time embedding + all block modulations for time t into mod (f32 [L][6][width]). */
 int f3c_op_modulation(const f3c_model* m, double t, float* mod_dev, float* scratch_dev /* 2*width f32 */,

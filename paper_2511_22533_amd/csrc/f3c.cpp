@@ -983,7 +983,7 @@ int f3c_op_gemm(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K
   if ((K * es) % 128) return fail(F3C_EINVAL, "K must be a multiple of %d", 128 / es);
   if (lda < K || ldw < K || (lda * es) % 16 || (ldw * es) % 16) return fail(F3C_EINVAL, "bad leading dims");
   if (!A || !W || !bias) return fail(F3C_EINVAL, "NULL operand");
-  if (epilogue == 2 ? (!resid || ldr < N || ldr % 4) : (!out || ldo < N || ldo % 4))
+  if (epilogue == 2 ? ((M && !resid) || ldr < N || ldr % 4) : (!out || ldo < N || ldo % 4))
     return fail(F3C_EINVAL, "bad output (leading dim below N or not a multiple of 4)");
   HIP_TRY(launch_gemm(SITE_OP, dtype, epilogue, M, N, K, A, lda, W, ldw, bias, gate, out, ldo, resid, ldr,
                       (hipStream_t)stream));
@@ -1062,6 +1062,89 @@ static int segs_from_host(int32_t batch, const int32_t* off_host, int cap, Segs*
     if (b > 0 && (off_host[b] < off_host[b - 1] || off_host[b] - off_host[b - 1] > cap))
       return fail(F3C_EINVAL, "segment %d must hold 0..%d rows", b - 1, cap);
   }
+  return F3C_OK;
+}
+
+// Alignment of a pointer and of the rows behind it (ld elements of es bytes).
+static bool aligned_rows(const void* p, int64_t ld, int es, int to) {
+  return ((uintptr_t)p % to) == 0 && (ld * es) % to == 0;
+}
+
+// Scale bytes of ceil(cols / 128) blocks per row (no rows: no pointer either).
+static int check_scales(const char* what, const void* p, int64_t ld, int64_t cols, int64_t rows) {
+  if (!p && rows) return fail(F3C_EINVAL, "NULL %s", what);
+  if (ld < (cols + 127) / 128 || !aligned_rows(p, ld, 1, 4))
+    return fail(F3C_EINVAL, "%s: row stride below ceil(columns/128), or not 4-byte aligned", what);
+  return F3C_OK;
+}
+
+int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K, const void* x, int32_t ldx, void* q,
+                     int32_t ldq, void* scale, int32_t lds, f3c_stream stream) {
+  if (dtype != F3C_F32 && dtype != F3C_BF16) return fail(F3C_EINVAL, "bad dtype");
+  if (block_rows != 1 && block_rows != 128) return fail(F3C_EINVAL, "block_rows must be 1 or 128");
+  if (rows < 0 || K <= 0 || K % 8) return fail(F3C_EINVAL, "bad shape (K must be a multiple of 8)");
+  if (rows && (!x || !q)) return fail(F3C_EINVAL, "NULL argument");
+  if (ldx < K || ldq < K || !aligned_rows(x, ldx, dtype == F3C_BF16 ? 2 : 4, 16) || !aligned_rows(q, ldq, 1, 8))
+    return fail(F3C_EINVAL, "bad leading dims or alignment (x rows 16 bytes, q rows 8)");
+  if (int rc = check_scales("scale", scale, lds, K, rows)) return rc;
+  HIP_TRY(launch_quant_fp8(dtype, block_rows, rows, K, x, ldx, q, ldq, scale, lds, (hipStream_t)stream));
+  return F3C_OK;
+}
+
+int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,
+                    const void* A_scale, int32_t ldsa, const void* W, int32_t ldw, const void* W_scale, int32_t ldsw,
+                    const float* bias, const float* gate, void* out, int32_t ldo, void* out_scale, int32_t ldso,
+                    float* resid, int32_t ldr, f3c_stream stream) {
+  if (epilogue < EPI_STORE || epilogue > EPI_GELU_FP8) return fail(F3C_EINVAL, "bad epilogue");
+  if (M < 0 || N <= 0 || K <= 0) return fail(F3C_EINVAL, "bad shape");
+  if (N % 16 || K % 16) return fail(F3C_EINVAL, "N and K must be multiples of 16");
+  if ((M && !A) || !W) return fail(F3C_EINVAL, "NULL operand");
+  if (lda < K || ldw < K || !aligned_rows(A, lda, 1, 16) || !aligned_rows(W, ldw, 1, 16))
+    return fail(F3C_EINVAL, "bad leading dims or alignment of A or W");
+  if (lda >= (1 << 22) || ldw >= (1 << 22)) return fail(F3C_EINVAL, "rows of A and W must be closer than 2^22 bytes");
+  if (int rc = check_scales("A_scale", A_scale, ldsa, K, M)) return rc;
+  if (int rc = check_scales("W_scale", W_scale, ldsw, K, N)) return rc;
+  if ((bias && (uintptr_t)bias % 16) || (gate && (uintptr_t)gate % 16))
+    return fail(F3C_EINVAL, "bias and gate must be 16-byte aligned");
+  if (gate && epilogue != EPI_RESID) return fail(F3C_EINVAL, "gate goes with the residual epilogue");
+  if (epilogue == EPI_RESID ? ((M && !resid) || ldr < N || !aligned_rows(resid, ldr, 4, 16))
+                            : ((M && !out) || ldo < N || !aligned_rows(out, ldo, epilogue == EPI_GELU_FP8 ? 1 : 2, 16)))
+    return fail(F3C_EINVAL, "bad output (NULL, leading dim below N or rows not 16-byte aligned)");
+  if (epilogue == EPI_GELU_FP8)
+    if (int rc = check_scales("out_scale", out_scale, ldso, N, M)) return rc;
+  HIP_TRY(launch_gemm_fp8(epilogue, M, N, K, A, lda, A_scale, ldsa, W, ldw, W_scale, ldsw, bias, gate, out, ldo,
+                          out_scale, ldso, resid, ldr, (hipStream_t)stream));
+  return F3C_OK;
+}
+
+int f3c_op_resid_norm(const f3c_resid_norm_cfg* cfg, int32_t d, int32_t batch, const int32_t* off_host, const void* y,
+                      int32_t ldy, const float* post_w, const float* gate, float* h, int32_t ldh, const float* pre_w,
+                      const float* shift, const float* scale, int32_t ldm, void* out, int32_t ldo, void* out_scale,
+                      int32_t lds, f3c_stream stream) {
+  if (!cfg) return fail(F3C_EINVAL, "NULL cfg");
+  if (cfg->dtype != F3C_F32 && cfg->dtype != F3C_BF16) return fail(F3C_EINVAL, "bad dtype");
+  if (cfg->out_dtype < F3C_F32 || cfg->out_dtype > F3C_FP8) return fail(F3C_EINVAL, "bad out_dtype");
+  if (cfg->post < NORM_NONE || cfg->post > NORM_RMS || cfg->pre < NORM_NONE || cfg->pre > NORM_RMS)
+    return fail(F3C_EINVAL, "bad norm");
+  if (!(cfg->eps > 0.0f) || !std::isfinite(cfg->eps) || !std::isfinite(cfg->resid_scale))
+    return fail(F3C_EINVAL, "eps must be positive and finite, resid_scale finite");
+  if (d < 8 || d > 8192 || d % 8) return fail(F3C_EINVAL, "d must be a multiple of 8 in 8..8192");
+  Segs rows{};
+  if (int rc = segs_from_host(batch, off_host, INT32_MAX, &rows)) return rc;
+  const int n = rows.off[batch] - rows.off[0];
+  if ((n && !h) || ldh < d || !aligned_rows(h, ldh, 4, 16)) return fail(F3C_EINVAL, "bad rows of h");
+  const int es = cfg->dtype == F3C_BF16 ? 2 : 4, eo = cfg->out_dtype == F3C_FP8 ? 1 : cfg->out_dtype == F3C_BF16 ? 2 : 4;
+  if (y && (ldy < d || !aligned_rows(y, ldy, es, 16))) return fail(F3C_EINVAL, "bad rows of y");
+  if (out && (ldo < d || !aligned_rows(out, ldo, eo, eo == 1 ? 8 : 16))) return fail(F3C_EINVAL, "bad rows of out");
+  if (out && cfg->out_dtype == F3C_FP8)
+    if (int rc = check_scales("out_scale", out_scale, lds, d, n)) return rc;
+  if ((shift == nullptr) != (scale == nullptr)) return fail(F3C_EINVAL, "shift and scale go together");
+  if ((gate || scale) && ldm != 0 && (ldm < d || ldm % 4)) return fail(F3C_EINVAL, "ldm must be 0 or at least d");
+  for (const float* v : {post_w, gate, pre_w, shift, scale})
+    if (v && (uintptr_t)v % 16) return fail(F3C_EINVAL, "vectors must be 16-byte aligned");
+  HIP_TRY(launch_resid_norm(cfg->dtype, cfg->out_dtype, cfg->post, cfg->pre, cfg->eps, cfg->resid_scale, d, rows, y,
+                            ldy, post_w, gate, h, ldh, pre_w, shift, scale, ldm, out, ldo, out_scale, lds,
+                            (hipStream_t)stream));
   return F3C_OK;
 }
 

@@ -21,7 +21,8 @@ LIB_PATH = os.path.join(HERE, "lib", "libf3c.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "f3c.h")
 
 F3C_OK, F3C_EINVAL, F3C_ENOMEM, F3C_EHIP, F3C_ESTATE = 0, -1, -2, -3, -4
-F3C_F32, F3C_BF16 = 0, 1
+F3C_F32, F3C_BF16, F3C_FP8 = 0, 1, 2
+F3C_NORM_NONE, F3C_NORM_LAYER, F3C_NORM_RMS = 0, 1, 2
 F3C_STATE_GUIDED = 1
 PROF_CLASSES = ["select", "embed", "mod", "ln", "gemm_qkv", "attn_self", "gemm_o", "gemm_q", "attn_cross",
                 "gemm_co", "gemm_fc1", "gemm_fc2", "final", "euler", "cond"]
@@ -42,6 +43,11 @@ class F3CError(RuntimeError):
 class ModelCfg(ctypes.Structure):
     _fields_ = [(n, c_int) for n in ("grid", "in_ch", "width", "depth", "heads", "mlp_ratio", "cond_tokens",
                                      "cond_width", "dtype")]
+
+
+class ResidNormCfg(ctypes.Structure):
+    _fields_ = [("dtype", c_int), ("out_dtype", c_int), ("post", c_int), ("pre", c_int), ("eps", c_f),
+                ("resid_scale", c_f)]
 
 
 _SIGS = {
@@ -88,6 +94,11 @@ _SIGS = {
     "f3c_op_attention": (c_int, [c_int, c_int, c_int, c_int, P_i32, P_i32, c_p, c_int, c_p, c_int, c_p, c_int, c_p,
                                  c_int, c_p, c_sz, c_int, c_p]),
     "f3c_op_ln_mod": (c_int, [c_int, c_int, c_int, c_p, c_p, c_p, c_p, c_p]),
+    "f3c_op_quant_fp8": (c_int, [c_int, c_int, c_int, c_int, c_p, c_int, c_p, c_int, c_p, c_int, c_p]),
+    "f3c_op_gemm_fp8": (c_int, [c_int, c_int, c_int, c_int, c_p, c_int, c_p, c_int, c_p, c_int, c_p, c_int, c_p, c_p,
+                                c_p, c_int, c_p, c_int, c_p, c_int, c_p]),
+    "f3c_op_resid_norm": (c_int, [ctypes.POINTER(ResidNormCfg), c_int, c_int, P_i32, c_p, c_int, c_p, c_p, c_p, c_int,
+                                  c_p, c_p, c_p, c_int, c_p, c_int, c_p, c_int, c_p]),
     "f3c_op_modulation": (c_int, [c_p, c_d, c_p, c_p, c_p]),
     "f3c_op_embed": (c_int, [c_p, c_int, c_p, c_p, P_i32, c_p, c_p]),
     "f3c_op_final": (c_int, [c_p, c_int, c_p, c_p, c_p]),
@@ -519,3 +530,138 @@ def op_ln_mod(dtype: int, h, out, shift=None, scale=None, stream=None):
     rows, d = h.shape
     check(lib().f3c_op_ln_mod(dtype, rows, d, h.data_ptr(), _ptr(shift), _ptr(scale), out.data_ptr(),
                               _stream(stream)))
+
+
+# ------------------------------------------------------------- 8-bit operators
+
+def _rows(name: str, t, dtypes: Sequence, shape=None):
+    """t as rows for the C ABI: a 2-D tensor of one of these types with contiguous columns, on the current device."""
+    import torch
+    if t.dtype not in [getattr(torch, d) for d in dtypes]:
+        raise ValueError(f"{name}: {t.dtype}, expected {' or '.join(dtypes)}")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: rows with contiguous columns expected")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {tuple(t.shape)}, expected {tuple(shape)}")
+    return _on_device(name, t)
+
+
+def _on_device(name: str, t):
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, expected the current GPU")
+    return t
+
+
+def _vector(name: str, t, n: int):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: {n} contiguous float32 values expected")
+    return _on_device(name, t).data_ptr()
+
+
+def _ld(t) -> int:
+    """Row stride; of a single row (or none), whose stride says nothing, its length rounded up to 16 bytes."""
+    if t.shape[0] > 1:
+        return t.stride(0)
+    step = 16 // t.element_size()
+    return (t.shape[1] + step - 1) // step * step
+
+
+_FP8 = ("float8_e4m3fn", "uint8")
+_SCALE = ("float8_e8m0fnu", "uint8")
+_FLOAT = {F3C_F32: ("float32",), F3C_BF16: ("bfloat16",), F3C_FP8: _FP8}
+
+
+def _scale_rows(name: str, t, rows: int, cols: int):
+    _rows(name, t, _SCALE)
+    if t.shape[0] != rows or t.shape[1] < fp8_scale_stride(cols):
+        raise ValueError(f"{name}: {tuple(t.shape)}, expected [{rows}][{fp8_scale_stride(cols)} or more]")
+    return t
+
+
+def fp8_scale_stride(cols: int) -> int:
+    """Row stride of the scales of `cols` columns: one byte per block of 128, rounded up to 4."""
+    return ((cols + 127) // 128 + 3) // 4 * 4
+
+
+def op_quant_fp8(dtype: int, x, q, scale, block_rows: int = 1, stream=None):
+    """x [R][K] -> q (e4m3 [R][K]) and scale (E8M0 bytes [ceil(R / block_rows)][fp8_scale_stride(K)])."""
+    if dtype not in (F3C_F32, F3C_BF16) or block_rows not in (1, 128):
+        raise ValueError("dtype F3C_F32 or F3C_BF16, block_rows 1 or 128")
+    _rows("x", x, _FLOAT[dtype])
+    R, K = x.shape
+    _rows("q", q, _FP8, (R, K))
+    _scale_rows("scale", scale, (R + block_rows - 1) // block_rows, K)
+    check(lib().f3c_op_quant_fp8(dtype, block_rows, R, K, x.data_ptr(), _ld(x), q.data_ptr(), _ld(q),
+                                 scale.data_ptr(), _ld(scale), _stream(stream)))
+
+
+def op_gemm_fp8(epilogue: int, A, A_scale, W, W_scale, bias=None, out=None, out_scale=None, resid=None, gate=None,
+                stream=None):
+    """op_gemm on 8-bit operands (op_quant_fp8's: A per row, W with block_rows 128). Epilogue 3 writes GELU as 8-bit
+    rows: out e4m3 and out_scale."""
+    if epilogue not in (0, 1, 2, 3):
+        raise ValueError("epilogue 0..3 expected")
+    _rows("A", A, _FP8)
+    M, K = A.shape
+    N = W.shape[0]
+    _rows("W", W, _FP8, (N, K))
+    _scale_rows("A_scale", A_scale, M, K)
+    _scale_rows("W_scale", W_scale, (N + 127) // 128, K)
+    if epilogue == 2:
+        if resid is None or out is not None or out_scale is not None:
+            raise ValueError("epilogue 2 updates resid alone")
+        _rows("resid", resid, ("float32",), (M, N))
+    else:
+        if out is None or resid is not None or (out_scale is None) != (epilogue != 3):
+            raise ValueError("epilogues 0 and 1 write out, 3 out and out_scale")
+        _rows("out", out, _FP8 if epilogue == 3 else ("bfloat16",), (M, N))
+        if epilogue == 3:
+            _scale_rows("out_scale", out_scale, M, N)
+    opt = lambda t: (None, 0) if t is None else (t.data_ptr(), _ld(t))  # noqa: E731
+    check(lib().f3c_op_gemm_fp8(epilogue, M, N, K, A.data_ptr(), _ld(A), A_scale.data_ptr(), _ld(A_scale),
+                                W.data_ptr(), _ld(W), W_scale.data_ptr(), _ld(W_scale), _vector("bias", bias, N),
+                                _vector("gate", gate, N), *opt(out), *opt(out_scale), *opt(resid), _stream(stream)))
+
+
+def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out_scale=None, post: int = F3C_NORM_NONE,
+                  pre: int = F3C_NORM_LAYER, post_w=None, pre_w=None, gate=None, resid_scale: float = 1.0, shift=None,
+                  scale=None, eps: float = 1e-6, stream=None):
+    """The pass between two blocks: h += resid_scale * gate * (post(y) * post_w), out = (pre(h) * pre_w) * (1 + scale)
+    + shift. off: row offsets of the samples (default: one sample of all rows); gate, shift, scale [B][d], or [d] for
+    all samples. y None: the norm alone; out None: the update alone."""
+    if dtype not in (F3C_F32, F3C_BF16) or out_dtype not in _FLOAT:
+        raise ValueError("dtype F3C_F32 or F3C_BF16, out_dtype F3C_F32, F3C_BF16 or F3C_FP8")
+    _rows("h", h, ("float32",))
+    R, d = h.shape
+    off = [0, R] if off is None else [int(v) for v in off]
+    B = len(off) - 1
+    if B < 1 or off[-1] > R:
+        raise ValueError("off: B + 1 row offsets within h expected")
+    if y is not None:
+        _rows("y", y, _FLOAT[dtype], (R, d))
+    if out is not None:
+        _rows("out", out, _FLOAT[out_dtype], (R, d))
+        if (out_scale is None) != (out_dtype != F3C_FP8):
+            raise ValueError("out_scale goes with F3C_FP8 rows")
+        if out_scale is not None:
+            _scale_rows("out_scale", out_scale, R, d)
+    mods = [(n, t) for n, t in (("gate", gate), ("shift", shift), ("scale", scale)) if t is not None]
+    ldm = None
+    for name, t in mods:
+        if t.dim() == 1:
+            _vector(name, t, d)
+        else:
+            _rows(name, t, ("float32",), (B, d))
+        ld = 0 if t.dim() == 1 or B == 1 else t.stride(0)
+        if ldm is not None and ld != ldm:
+            raise ValueError("gate, shift and scale must have one row stride")
+        ldm = ld
+    c = ResidNormCfg(dtype, out_dtype, post, pre, eps, resid_scale)
+    opt = lambda t: (None, 0) if t is None else (t.data_ptr(), _ld(t))  # noqa: E731
+    check(lib().f3c_op_resid_norm(ctypes.byref(c), d, B, _i32(off), *opt(y), _vector("post_w", post_w, d), _ptr(gate),
+                                  h.data_ptr(), _ld(h), _vector("pre_w", pre_w, d), _ptr(shift), _ptr(scale),
+                                  ldm or 0, *opt(out), *opt(out_scale), _stream(stream)))
