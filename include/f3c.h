@@ -416,7 +416,7 @@ int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K,
  * adds the products of 8 consecutive k after aligning them to their largest and
  * drops bits 2^14 below it, so a sum of n normally distributed products is about
  * 1.3e-5 of its size off. N and K multiples of 16; rows of A, W, out and resid
- * 16-byte aligned, of bias and gate too; lda and ldw below 2^22. The result of an
+ * 16-byte aligned, of bias and gate too; lda, ldw, ldsa, ldsw below 2^22. The result of an
  * output row does not depend on M or on other rows, nor on scheduling. out,
  * out_scale and resid must not overlap the operands. Errors: F3C_EINVAL. */
 int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,

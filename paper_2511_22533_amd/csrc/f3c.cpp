@@ -1101,7 +1101,8 @@ int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const voi
   if ((M && !A) || !W) return fail(F3C_EINVAL, "NULL operand");
   if (lda < K || ldw < K || !aligned_rows(A, lda, 1, 16) || !aligned_rows(W, ldw, 1, 16))
     return fail(F3C_EINVAL, "bad leading dims or alignment of A or W");
-  if (lda >= (1 << 22) || ldw >= (1 << 22)) return fail(F3C_EINVAL, "rows of A and W must be closer than 2^22 bytes");
+  for (int32_t ld : {lda, ldsa, ldw, ldsw})
+    if (ld >= (1 << 22)) return fail(F3C_EINVAL, "rows of the operands and their scales must be below 2^22 bytes");
   if (int rc = check_scales("A_scale", A_scale, ldsa, K, M)) return rc;
   if (int rc = check_scales("W_scale", W_scale, ldsw, K, N)) return rc;
   if ((bias && (uintptr_t)bias % 16) || (gate && (uintptr_t)gate % 16))

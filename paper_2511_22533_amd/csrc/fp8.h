@@ -29,20 +29,23 @@ __device__ __forceinline__ uint32_t fp8_scale_byte(float amax) {
   return (uint32_t)(e < 1 ? 1 : e);
 }
 
-// 2^-e of a scale byte (1..247 by construction: a normal number).
-__device__ __forceinline__ float fp8_inverse(uint32_t byte) {
-  return __builtin_bit_cast(float, (254u - byte) << 23);
+// 2^e of a scale byte (1..247 by construction: a normal number).
+__device__ __forceinline__ float fp8_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Four finite values or NaNs over 2^e (the scale as a float) as e4m3 bytes, the
+// first in the lowest: the conversion divides by the scale, exactly, and rounds
+// once, to nearest even; nothing is out of range of a scale of fp8_scale_byte.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d, float scale) {
+  s16x2 w{0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, w);
 }
 
-// Four values, times inv, as e4m3 bytes (the first in the lowest). An infinity
-// is turned into NaN first: what the conversion makes of it is a mode's choice.
-__device__ __forceinline__ uint32_t fp8_pack4(float a, float b, float c, float d, float inv) {
-  auto one = [inv](float x) {
-    x *= inv;
-    return __builtin_fabsf(x) <= 448.0f ? x : __builtin_nanf("");
-  };
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(one(a), one(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(one(c), one(d), w, true);
+// x, an infinity as NaN (what the conversion makes of it is a mode's choice).
+__device__ __forceinline__ float fp8_no_inf(float x) {
+  return __builtin_fabsf(x) < __builtin_inff() ? x : __builtin_nanf("");
 }
 
 // Largest of v over each row of 16 lanes, in all of them.

@@ -43,8 +43,12 @@ __device__ __forceinline__ float amax8(const float (&v)[8]) {
   return m;
 }
 
-__device__ __forceinline__ void store8_fp8(uint8_t* p, const float (&v)[8], float inv) {
-  *reinterpret_cast<u32x2*>(p) = u32x2{fp8_pack4(v[0], v[1], v[2], v[3], inv), fp8_pack4(v[4], v[5], v[6], v[7], inv)};
+__device__ __forceinline__ void store8_fp8(uint8_t* p, const float (&v)[8], float scale) {
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = fp8_no_inf(v[e]);
+  *reinterpret_cast<u32x2*>(p) =
+      u32x2{fp8_pack4(x[0], x[1], x[2], x[3], scale), fp8_pack4(x[4], x[5], x[6], x[7], scale)};
 }
 
 // Blocks of 1 x 128: a lane holds 8 columns, 16 lanes a block, a wave 512 columns
@@ -62,7 +66,7 @@ __global__ __launch_bounds__(256) void k_quant_rows(const T* __restrict__ x, int
   if (in) r = load8(x + row * ldx + c);
   const uint32_t byte = fp8_scale_byte(row16_max(amax8(r.v)));
   if (!in) return;
-  store8_fp8(q + row * ldq + c, r.v, fp8_inverse(byte));
+  store8_fp8(q + row * ldq + c, r.v, fp8_scale(byte));
   if ((lane & 15) == 0) scale[row * lds + c / kFp8Block] = (uint8_t)byte;
 }
 
@@ -90,10 +94,10 @@ __global__ __launch_bounds__(256) void k_quant_tiles(const T* __restrict__ x, in
   if ((tid & 63) == 0) part[tid >> 6] = m;
   __syncthreads();
   const uint32_t byte = fp8_scale_byte(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
-  const float inv = fp8_inverse(byte);
+  const float two_e = fp8_scale(byte);
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (c < K && r0 + 16 * i < rows) store8_fp8(q + (r0 + 16 * i) * ldq + c, r[i].v, inv);
+    if (c < K && r0 + 16 * i < rows) store8_fp8(q + (r0 + 16 * i) * ldq + c, r[i].v, two_e);
   if (tid == 0) scale[by * lds + bx] = (uint8_t)byte;
 }
 
@@ -219,7 +223,7 @@ __global__ __launch_bounds__(256) void k_resid_norm(ResidNormArgs p) {
     if constexpr (OUT == DT_FP8) {
       const uint32_t byte = fp8_scale_byte(row16_max(amax8(h[j])));   // (0 past the row's end)
       if (c < p.d) {
-        store8_fp8(reinterpret_cast<uint8_t*>(p.out) + row * p.ldo + c, h[j], fp8_inverse(byte));
+        store8_fp8(reinterpret_cast<uint8_t*>(p.out) + row * p.ldo + c, h[j], fp8_scale(byte));
         if ((lane & 15) == 0) p.out_scale[row * p.lds + c / kFp8Block] = (uint8_t)byte;
       }
     } else if (c < p.d) {

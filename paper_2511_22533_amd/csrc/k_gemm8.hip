@@ -13,6 +13,9 @@
 // alike, 2000 times below the operands' own rounding. No instruction that takes
 // 8-bit operands does otherwise (16x16x32, 16x16x128 and 32x32x64 agree bit for
 // bit); the bf16 ones do, at half the rate.
+#include <algorithm>
+#include <cmath>
+
 #include "fp8.h"
 #include "kernels.h"
 
@@ -38,91 +41,543 @@ struct Gemm8Args {
   int64_t ldso;
   float* resid;
   int64_t ldr;
+  int xq;                             // column groups of the XCD tile partition
 };
 
-// Few rows: fragments straight from memory. A wave multiplies 16 weight rows (the
-// instruction's A operand, so that a lane ends with four consecutive columns of
-// one activation row) by 16 activation rows; 8 waves stand side by side over 128
-// columns.
-template <int EPI>
-__global__ __launch_bounds__(512) void k_gemm8_rows(Gemm8Args p) {
-  __shared__ float part[8][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
-  const int nb = (p.N + 127) / 128, block = blockIdx.x % nb;
-  const int n0 = block * 128 + wave * 16, m0 = (int)(blockIdx.x / nb) * 16;
-  const int KT = (p.K + 127) / 128;
-  const int am = min(m0 + r, p.M - 1), wn = min(n0 + r, p.N - 1);     // rows past the end re-read the last one
-  const uint8_t* a = p.A + am * p.lda;
-  const uint8_t* w = p.W + wn * p.ldw;
-  const uint8_t* sa = p.sa + am * p.ldsa;
-  const uint8_t* sw = p.sw + (wn >> 7) * p.ldsw;
-  f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};
-  union Frag { i32x8 v; u32x4 h[2]; };
-  for (int kt = 0; kt < KT; ++kt) {
-    Frag fa, fw;
+// GELU in its tanh form as x / (1 + 2^(x (a + b x^2))), a = -2 log2(e) sqrt(2/pi),
+// b = 0.044715 a: five operations, an exponential and a reciprocal.
+__device__ __forceinline__ float gelu_fast(float x) {
+  const float z = x * __builtin_fmaf(x * x, -0.10294324f, -2.3022082f);
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z));
+}
+
+// Epilogue through LDS, 32 rows of the wave at a time (a lane of the MFMA layout
+// holds four columns here and there of one row; rows leave in whole pieces). The
+// region is the wave's own and LDS operations of a wave keep their order. All of
+// the workgroup's LDS is free to use.
+template <int TM, int TN, int WTM, int WTN, int BM, int BN, int WGN, int BYTES, int EPI>
+__device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)[TM][TN], char* lds, int m0, int n0,
+                                               int wm, int wn, int lane) {
+  const int g = lane >> 5, r32 = lane & 31, wave = wm * WGN + wn;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  constexpr int NW = (BM / WTM) * WGN;
+  if constexpr (EPI == EPI_GELU_FP8) {
+    // A quantisation block is 128 columns of a row: the wave's own (WTN = 128), or
+    // spread over 128 / WTN waves, which meet in LDS.
+    constexpr int RS = WTN + 16;
+    constexpr int PARTS = 128 / WTN;
+    static_assert(NW * 32 * RS + WGN * BM * 4 <= BYTES && BN % 128 == 0, "epilogue buffer");
+    const int c0 = n0 + wn * WTN;
+    // largest magnitudes; an infinity among them (which a NaN cannot hide) is rare
+    // and turns into NaN in a second look
+    float top[TM];
+    bool odd = false;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int k = kt * 128 + (g + 4 * x) * 16;
-      fa.h[x] = fw.h[x] = u32x4{0, 0, 0, 0};
-      if (k < p.K) {
-        fa.h[x] = *reinterpret_cast<const u32x4*>(a + k);
-        fw.h[x] = *reinterpret_cast<const u32x4*>(w + k);
+    for (int i = 0; i < TM; ++i) {
+      float m = 0.0f;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = gelu_fast(acc[i][j][e]);
+      if (n0 + BN > p.N) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (c0 + j * 32 + 8 * (e / 4) + 4 * g >= p.N) acc[i][j][e] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)
+          m = fmaxf(fmaxf(m, __builtin_fabsf(acc[i][j][e])), __builtin_fabsf(acc[i][j][e + 1]));
+      top[i] = m;
+      odd = odd || !(m < __builtin_inff());
+    }
+    if (__any(odd)) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            m = fmaxf(m, finite_abs(acc[i][j][e]));
+            acc[i][j][e] = fp8_no_inf(acc[i][j][e]);
+          }
+        top[i] = m;
       }
     }
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw.v, fa.v, acc, 0, 0, 0, (int)sw[kt], 0, (int)sa[kt]);
-  }
-  const int row = m0 + r, col = n0 + 4 * g;
-  float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-  const bool in = row < p.M && col < p.N;
-  if (p.bias && col < p.N) {
-    const float4 b = *reinterpret_cast<const float4*>(p.bias + col);
-    v[0] += b.x, v[1] += b.y, v[2] += b.z, v[3] += b.w;
-  }
-  if constexpr (EPI == EPI_GELU || EPI == EPI_GELU_FP8) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
-  }
-  if constexpr (EPI == EPI_RESID) {
-    if (!in) return;
-    float4 gv = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-    if (p.gate) gv = *reinterpret_cast<const float4*>(p.gate + col);
-    float4* dst = reinterpret_cast<float4*>(p.resid + row * p.ldr + col);
-    float4 h = *dst;
-    h.x += gv.x * v[0];
-    h.y += gv.y * v[1];
-    h.z += gv.z * v[2];
-    h.w += gv.w * v[3];
-    *dst = h;
-  } else if constexpr (EPI == EPI_GELU_FP8) {
-    float m = 0.0f;
-    if (col < p.N) {
+    for (int i = 0; i < TM; ++i) top[i] = fmaxf(top[i], __shfl_xor(top[i], 32));
+    if constexpr (PARTS > 1) {
+      float* part = reinterpret_cast<float*>(lds + NW * 32 * RS);      // [WGN][BM]
+      if (g == 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) m = fmaxf(m, finite_abs(v[e]));
+        for (int i = 0; i < TM; ++i) part[wn * BM + wm * WTM + i * 32 + r32] = top[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x)
+          top[i] = fmaxf(top[i], part[(wn / PARTS * PARTS + x) * BM + wm * WTM + i * 32 + r32]);
     }
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    if (g == 0) part[wave][r] = m;
-    __syncthreads();
+    const uint32_t eb = lds0 + (uint32_t)(wave * 32 * RS);
+    typedef __attribute__((address_space(3))) uint32_t lds_w;
+    typedef __attribute__((address_space(3))) const u32x4 lds_r;
+    constexpr int LPR = WTN / 16, RPI = 64 / LPR;
 #pragma unroll
-    for (int x = 0; x < 8; ++x) m = fmaxf(m, part[x][r]);
-    if (!in) return;
-    const uint32_t byte = fp8_scale_byte(m);
-    *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(p.out) + row * p.ldo + col) =
-        fp8_pack4(v[0], v[1], v[2], v[3], fp8_inverse(byte));
-    if (wave == 0 && g == 0) p.so[row * p.ldso + block] = (uint8_t)byte;
+    for (int i = 0; i < TM; ++i) {
+      const uint32_t byte = fp8_scale_byte(top[i]);
+      const float two_e = fp8_scale(byte);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(lds_w*)(uintptr_t)(eb + (uint32_t)(r32 * RS + j * 32 + 8 * q + 4 * g)) =
+              fp8_pack4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3], two_e);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const int row0 = m0 + wm * WTM + i * 32;
+      if (g == 0 && wn % PARTS == 0 && row0 + r32 < p.M && c0 < p.N)
+        p.so[(row0 + r32) * p.ldso + (c0 >> 7)] = (uint8_t)byte;
+      const int ecol = c0 + (lane % LPR) * 16;
+#pragma unroll
+      for (int t = 0; t < 32 / RPI; ++t) {
+        const int rr = t * RPI + lane / LPR, row = row0 + rr;
+        const u32x4 v = *(lds_r*)(uintptr_t)(eb + (uint32_t)(rr * RS + (lane % LPR) * 16));
+        if (row < p.M && ecol < p.N)
+          *reinterpret_cast<u32x4*>(reinterpret_cast<uint8_t*>(p.out) + row * p.ldo + ecol) = v;
+      }
+    }
   } else {
-    if (!in) return;
-    bf16x4 o;
+  constexpr int RS = WTN * 4 + 16;
+  static_assert(NW * 32 * RS <= BYTES, "epilogue buffer");
+  typedef __attribute__((address_space(3))) f32x4 lds_f4;
+  const uint32_t eb = lds0 + (uint32_t)(wave * 32 * RS);
+  // columns per lane, lanes per row, rows per pass
+  constexpr int VC = EPI == EPI_RESID ? 4 : 8, LPR = WTN / VC, RPI = 64 / LPR;
+  const int ecol = n0 + wn * WTN + (lane % LPR) * VC;
+  const bool in = ecol < p.N;                      // all VC columns or none
+  float gv[VC];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (bf16)v[e];
-    *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16*>(p.out) + row * p.ldo + col) = o;
+  for (int e = 0; e < VC; e += 4) {
+    float4 g4 = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+    if (EPI == EPI_RESID && p.gate && in) g4 = *reinterpret_cast<const float4*>(p.gate + ecol + e);
+    gv[e] = g4.x, gv[e + 1] = g4.y, gv[e + 2] = g4.z, gv[e + 3] = g4.w;
   }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(lds_f4*)(uintptr_t)(eb + (uint32_t)(r32 * RS + (j * 32 + 8 * q + 4 * g) * 4)) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int row0 = m0 + wm * WTM + i * 32 + lane / LPR;
+#pragma unroll
+    for (int t = 0; t < 32 / RPI; ++t) {
+      const int row = row0 + t * RPI;
+      float v[VC];
+#pragma unroll
+      for (int e = 0; e < VC; e += 4) {
+        const uint32_t at = eb + (uint32_t)((t * RPI + lane / LPR) * RS + ((lane % LPR) * VC + e) * 4);
+        const f32x4 c4 = *(lds_f4*)(uintptr_t)at;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[e + x] = c4[x];
+      }
+      if (row >= p.M || !in) continue;
+      if constexpr (EPI == EPI_RESID) {
+        float4* r = reinterpret_cast<float4*>(p.resid + row * p.ldr + ecol);
+        float4 h = *r;
+        h.x += gv[0] * v[0];
+        h.y += gv[1] * v[1];
+        h.z += gv[2] * v[2];
+        h.w += gv[3] * v[3];
+        *r = h;
+      } else {
+        bf16x8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if constexpr (EPI == EPI_GELU) v[e] = gelu_fast(v[e]);
+          o[e] = (bf16)v[e];
+        }
+        *reinterpret_cast<bf16x8*>(reinterpret_cast<bf16*>(p.out) + row * p.ldo + ecol) = o;
+      }
+    }
+  }
+  }
+}
+
+// Many rows: K tiles of 128 bytes (one scale block) go HBM -> LDS by DMA into
+// STAGES stages; each wave multiplies TM x TN tiles of 32 x 32 on 32x32x64
+// instructions, two K-steps per tile.
+//
+// The weight fragment is the instruction's A operand and the activation fragment
+// its B operand (a tile of C^T), as in the bf16 kernels. A lane feeds 32 bytes of
+// one row per instruction: 16-byte chunks g and g + 2 of the K-step's four, so
+// that the instruction adds the 8-byte groups in the order of K.
+//
+// Activation fragments roll: fragment i of the next K-step is read as soon as its
+// last product of this one is issued. Weight fragments, needed until the end, are
+// read a K-step ahead into a second set.
+//
+// Scales come with their K tile: the dword of each row that holds the tile's byte,
+// by DMA too, shifted into place as it is read. The loop over K has no branch: the
+// compiler would move products across it, out of their places between the reads.
+template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1>
+__global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
+  constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
+  constexpr int KTB = 128, ABUF = BM * KTB, SBUF = (BM + BN) * KTB;
+  constexpr int DA = BM / 8, DB = BN / 8, DQ = (DA + DB) / NW;         // DMA blocks of 8 rows
+  constexpr int SA = (BM + 63) / 64, SX = (SA + NW) / NW, DT = DQ + SX;       // scale DMAs: of A, and per wave; all of a wave
+  constexpr int SSET = 64 * NW * SX * 4;                               // bytes of a stage's scales
+  static_assert(DA % NW == 0 && DB % NW == 0, "whole DMA blocks per wave");
+  static_assert(BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0 && WTN <= 128 && NW % 2 == 0, "tile shape");
+  constexpr int EB = EPI == EPI_GELU_FP8 ? NW * 32 * (WTN + 16) + WGN * BM * 4 : NW * 32 * (WTN * 4 + 16);
+  constexpr int LDSB = STAGES * (SBUF + SSET) > EB ? STAGES * (SBUF + SSET) : EB;
+  __shared__ __attribute__((aligned(16))) char lds[LDSB];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WGN, wn = wave % WGN;
+  const int g = lane >> 5, r32 = lane & 31;
+  int n0, m0;
+  {
+    const int gx = (p.N + BN - 1) / BN, gy = (p.M + BM - 1) / BM;
+    const int l = xcd_logical_id(blockIdx.x, gx * gy);
+    const int gq = gx / p.xq, per_group = gy * gq;
+    const int grp = l / per_group, r = l - grp * per_group;
+    const int y = r / gq;
+    n0 = (grp * gq + (r - y * gq)) * BN;
+    m0 = y * BM;
+  }
+  const int KT = (p.K + KTB - 1) / KTB;
+  auto swizzle = [](int row) { return (row >> 1) & 7; };
+  // Descriptors span 2 GiB: an offset of 2^31 is out of range and reads zeros
+  // (chunks beyond K).
+  auto descriptor = [](const void* base) {
+    const uint64_t a = (uint64_t)base;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32) & 0xffffu), 0x80000000u, 0x00020000u};
+  };
+  const u32x4 adesc = descriptor(p.A + m0 * p.lda), wdesc = descriptor(p.W + n0 * p.ldw);
+  // DMA instruction q of this wave fills the 8 rows of block wave + NW q (A's
+  // blocks first): lane l row l/8 at physical chunk l%8, with the logical chunk
+  // that the row's swizzle maps there (the same for all q: a wave's blocks are all
+  // even or all odd). Rows past the end re-read the last one (never stored).
+  const int chunk = (lane % 8 ^ swizzle(8 * wave + lane / 8)) << 4;
+  uint32_t dofs[DQ];
+#pragma unroll
+  for (int q = 0; q < DQ; ++q) {
+    const int blk = wave + NW * q;
+    if (q < DA / NW) dofs[q] = (uint32_t)min(8 * blk + lane / 8, p.M - 1 - m0) * (uint32_t)p.lda + chunk;
+    else dofs[q] = (uint32_t)min(8 * (blk - DA) + lane / 8, p.N - 1 - n0) * (uint32_t)p.ldw + chunk;
+    asm("" : "+v"(dofs[q]));
+  }
+  auto cut_tail = [&](int t) {                     // what of K tile t on lies beyond K
+    const uint32_t m = t * KTB + chunk >= p.K ? 0x80000000u : 0u;
+#pragma unroll
+    for (int q = 0; q < DQ; ++q) dofs[q] |= m;
+  };
+  // Scale DMA x < SA: 64 rows of A from 64 x on; SA: the weight blocks of the
+  // tile's columns (those beyond it repeat SA's in places of their own). Wave w
+  // issues w, w + NW, ...
+  u32x4 sdesc[SX];
+  uint32_t sofs[SX];
+#pragma unroll
+  for (int y = 0; y < SX; ++y) {
+    const int x = wave + NW * y;
+    sdesc[y] = x < SA ? descriptor(p.sa + m0 * p.ldsa) : descriptor(p.sw + (n0 >> 7) * p.ldsw);
+    sofs[y] = x < SA ? (uint32_t)min(64 * x + lane, p.M - 1 - m0) * (uint32_t)p.ldsa
+                     : (uint32_t)min(lane, ((p.N - 1) >> 7) - (n0 >> 7)) * (uint32_t)p.ldsw;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  // DMA instruction q of K tile t (t < KT)
+  auto fetch1 = [&](int q, int t, int stage) {
+    const uint32_t k = (uint32_t)t * KTB;
+    if (q < DQ) {
+      const uint32_t dst = lds0 + (uint32_t)(stage * SBUF + (wave + NW * q) * 1024);
+      if (q < DA / NW) {
+        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+                     : : "v"(dofs[q]), "s"(adesc), "s"(k), "{m0}"(dst) : "memory");
+      } else {
+        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+                     : : "v"(dofs[q]), "s"(wdesc), "s"(k), "{m0}"(dst) : "memory");
+      }
+    } else {
+      const int y = q - DQ;
+      const uint32_t dst = lds0 + (uint32_t)(STAGES * SBUF + stage * SSET + (wave + NW * y) * 256), ks = (uint32_t)(t & ~3);
+      asm volatile("buffer_load_dword %0, %1, %2 offen lds"
+                   : : "v"(sofs[y]), "s"(sdesc[y]), "s"(ks), "{m0}"(dst) : "memory");
+    }
+  };
+  typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+  typedef __attribute__((address_space(3))) const uint32_t lds_u32;
+  uint32_t aad[2][2], wad[2][2];                   // K-step, chunk
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t ch = (uint32_t)(((4 * ks + 2 * x + g) ^ swizzle(r32)) << 4);
+      aad[ks][x] = lds0 + (wm * WTM + r32) * KTB + ch;
+      wad[ks][x] = lds0 + ABUF + (wn * WTN + r32) * KTB + ch;
+      asm("" : "+v"(aad[ks][x]), "+v"(wad[ks][x]));
+    }
+  f32x16 acc[TM][TN];                              // from the bias on
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int col = n0 + wn * WTN + j * 32 + 8 * q + 4 * g;
+      f32x4 b{0.0f, 0.0f, 0.0f, 0.0f};
+      if (p.bias && col < p.N) b = *reinterpret_cast<const f32x4*>(p.bias + col);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = b[e];
+    }
+  union Frag { i32x8 v; u32x4 h[2]; };
+  Frag fa[TM], fw[2][TN];
+  uint32_t sa[TM], sw, nsa[TM], nsw;
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  auto read_a = [&](int i, int ks) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) fa[i].h[x] = *(lds_u32x4*)(uintptr_t)(aad[ks][x] + (uint32_t)(i * 32 * KTB));
+  };
+  auto read_w = [&](int j, int ks) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) fw[ks][j].h[x] = *(lds_u32x4*)(uintptr_t)(wad[ks][x] + (uint32_t)(j * 32 * KTB));
+  };
+  const uint32_t sad = lds0 + (uint32_t)(STAGES * SBUF + (wm * WTM + r32) * 4);
+  const uint32_t swd = lds0 + (uint32_t)(STAGES * SBUF + (64 * SA + (((n0 & 127) + wn * WTN) >> 7)) * 4);
+  auto read_scales = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) nsa[i] = *(lds_u32*)(uintptr_t)(sad + (uint32_t)(stage * SSET + i * 128));
+    nsw = *(lds_u32*)(uintptr_t)(swd + (uint32_t)(stage * SSET));
+  };
+  auto take_scales = [&](int t) {                  // the byte of K tile t lowest
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = nsa[i] >> (8 * (t & 3));
+    sw = nsw >> (8 * (t & 3));
+  };
+  constexpr int GS = TM * TN;
+  auto product = [&](int ks, int i, int j) {
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[ks][j].v, fa[i].v, acc[i][j], 0, 0, 0, (int)sw, 0,
+                                                                (int)sa[i]);
+    fence();
+  };
+  if constexpr (STAGES == 1) {
+    auto open = [&](int t) {                       // K tile t has been issued: wait, read its first K-step
+      wait_vm<0>();
+      __builtin_amdgcn_s_barrier();
+      fence();
+      read_scales(0);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) read_w(j, 0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) read_a(i, 0);
+      take_scales(t);
+      fence();
+    };
+    cut_tail(0);
+#pragma unroll
+    for (int q = 0; q < DT; ++q) fetch1(q, 0, 0);
+    open(0);
+    for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          product(0, i, j);
+          if (j == TN - 1) read_a(i, 1);
+          if (i == 0) read_w(j, 1);
+          fence();
+        }
+      const int t = min(kt + 1, KT - 1);
+      cut_tail(kt + 1);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const int n = i * TN + j;
+          product(1, i, j);
+          if (n == TN - 1) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0): this wave holds the tile's last fragments
+            __builtin_amdgcn_s_barrier();
+            fence();
+          }
+          if (n >= TN - 1) {
+#pragma unroll
+            for (int q = 0; q < DT; ++q)
+              if (n == (TN - 1 + q / DPI < GS - 1 ? TN - 1 + q / DPI : GS - 1)) fetch1(q, t, 0);
+          }
+          fence();
+        }
+      open(kt + 1);
+    }
+  } else {
+  // After the barrier that frees tile kt's stage (behind product TN - 1 of its
+  // second K-step), tile kt + STAGES goes into it: over the rest of that K-step,
+  // and with more than two stages over the next one as well.
+  constexpr int SLOTS = GS - TN + 1 + (STAGES > 2 ? GS : 0), FAST = (DT + DPI - 1) / DPI < SLOTS ? (DT + DPI - 1) / DPI : SLOTS;
+  auto slot = [](int q) { return q * FAST / DT; };
+  auto wpos = [](int f, int from) { return from + f * (GS - from) / TN; };
+  int stage = 0, dstage = STAGES - 1, dt = min(STAGES - 1, KT - 1);
+  constexpr int EARLY = [] {                       // a tile's instructions within its first K-step's slots
+    int n = 0;
+    for (int q = 0; q < DT; ++q) n += q * FAST / DT < GS - TN + 1;
+    return n;
+  }();
+#pragma unroll
+  for (int s = 0; s < STAGES; ++s) {
+    cut_tail(s);
+#pragma unroll
+    for (int q = 0; q < DT; ++q)
+      if (s < STAGES - 1 || q < EARLY) fetch1(q, min(s, KT - 1), s);
+  }
+  wait_vm<(STAGES - 2) * DT + EARLY>();
+  __syncthreads();
+  // (in the loop's order, so that the compiler's waits in it are exact)
+  read_scales(0);
+#pragma unroll
+  for (int n = TN - 1; n < GS; ++n) {
+    if (n % TN == TN - 1) read_a(n / TN, 0);
+#pragma unroll
+    for (int f = 0; f < TN; ++f)
+      if (n == wpos(f, TN - 1)) read_w(f, 0);
+    fence();
+  }
+  take_scales(0);
+  fence();
+  for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const int n = i * TN + j, nxt = ks ^ 1;
+          product(ks, i, j);
+          if (ks == 1 && n == TN - 1) {
+            // every wave holds this tile's last fragments and tile kt + 1 has
+            // landed: one barrier retires tile kt's stage and opens kt + 1's
+            __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
+            wait_vm<(STAGES - 2) * DT>();
+            __builtin_amdgcn_s_barrier();
+            fence();
+            dstage = stage;
+            dt = min(kt + STAGES, KT - 1);
+            cut_tail(kt + STAGES);
+            const uint32_t d = stage == STAGES - 1 ? (uint32_t)(-(STAGES - 1) * SBUF) : (uint32_t)SBUF;
+            stage = stage == STAGES - 1 ? 0 : stage + 1;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                aad[k][x] += d;
+                wad[k][x] += d;
+              }
+            read_scales(stage);
+            fence();
+          }
+          if (j == TN - 1) read_a(i, nxt);
+          // the next K-step's weights: from this one's start, or from the barrier on
+#pragma unroll
+          for (int f = 0; f < TN; ++f)
+            if (n == wpos(f, ks == 1 ? TN - 1 : 0)) read_w(f, nxt);
+#pragma unroll
+          for (int q = 0; q < DT; ++q)
+            if (slot(q) == (ks == 1 ? n - (TN - 1) : n + GS - TN + 1) && (ks == 1 || STAGES > 2)) fetch1(q, dt, dstage);
+          fence();
+        }
+      if (ks == 1) take_scales(kt + 1);
+    }
+  }
+  }
+  wait_vm<0>();
+  __syncthreads();                                 // no DMA in flight, every wave past its last fragment read
+  gemm8_epilogue<TM, TN, WTM, WTN, BM, BN, WGN, LDSB, EPI>(p, acc, lds, m0, n0, wm, wn, lane);
+}
+
+// Column groups of the XCD tile partition (as the bf16 projections choose it).
+inline int choose_xq(int M, int N, int K, int BM, int BN) {
+  const int gx = (N + BN - 1) / BN;
+  const double a = (double)M * K, w = (double)N * K, l2_share = 2.0 * 1024 * 1024;
+  const double rounds = std::max(1.0, (double)((M + BM - 1) / BM) * gx / 256.0);
+  int best = 1;
+  double best_cost = 0.0;
+  for (int q = 1; q <= 8; q *= 2) {
+    if (gx % q) continue;
+    const double cost = a * q + (w / q <= l2_share ? w * (8.0 / q) : 8.0 * rounds * (w / q));
+    if (q == 1 || cost < best_cost) {
+      best = q;
+      best_cost = cost;
+    }
+  }
+  return best;
+}
+
+template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 2>
+hipError_t launch_dma(const Gemm8Args& a0, hipStream_t s) {
+  Gemm8Args a = a0;
+  a.xq = choose_xq(a.M, a.N, a.K, BM, BN);
+  const int64_t tiles = (int64_t)((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM);
+  launch((k_gemm8_dma<BM, BN, WGM, WGN, STAGES, OCC, EPI, DPI>), dim3((uint32_t)tiles), dim3(64 * WGM * WGN), 0, s, a);
+  return hipGetLastError();
+}
+
+// Tile shapes by a cost model in us, as the bf16 projections': a fixed cost, per K
+// tile a fixed cost, a cost per round of 256 x (workgroups per CU) workgroups (a
+// partial round costs a whole one) and one per 256 workgroups' load, and per round
+// and load the epilogue; a least-squares fit to 1374 measured calls on MI355X.
+struct Tile8Cost { int bm, bn, per_cu; double fixed, k, k_round, k_load, round, load_store, load_gelu, load_resid, load_fp8; };
+constexpr Tile8Cost kTile8Cost[] = {
+    {256, 256, 1, 1.911, 0.408, 0.668, 0.790, 4.769, 2.438, 7.088, 19.766, 6.991},
+    {128, 256, 2, 1.019, 0.843, 0.042, 0.748, 4.297, 0.966, 2.693, 10.072, 2.110},
+    {128, 128, 3, 1.924, 0.477, 0.118, 0.426, 2.067, 0.742, 1.477, 4.542, 1.073},
+    {128, 128, 1, 1.572, 0.071, 0.289, 0.330, 2.656, 0.000, 1.004, 3.680, 1.141},
+    {64, 128, 2, 1.835, 0.094, 0.273, 0.258, 1.712, 0.172, 0.608, 2.082, 0.425},
+    {32, 128, 1, 1.992, 0.000, 0.223, 0.123, 2.051, 0.000, 0.456, 1.112, 0.601},
+    {32, 128, 2, 1.969, 0.000, 0.308, 0.178, 1.088, 0.000, 0.351, 0.807, 0.268},
+    {32, 64, 2, 1.613, 0.000, 0.183, 0.092, 1.787, 0.000, 0.300, 0.558, 0.000},
+};
+
+inline int choose_tiles(int M, int N, int K, int epi) {
+  int best = -1;
+  double best_t = 0.0;
+  for (int c = 0; c < (int)(sizeof(kTile8Cost) / sizeof(kTile8Cost[0])); ++c) {
+    const Tile8Cost& m = kTile8Cost[c];
+    if (epi == EPI_GELU_FP8 && m.bn < kFp8Block) continue;             // a quantisation block in one workgroup
+    const double tiles = std::ceil((double)M / m.bm) * std::ceil((double)N / m.bn), load = tiles / 256.0;
+    const double rounds = std::ceil(load / m.per_cu), kt = std::ceil(K / 128.0);
+    const double t = m.fixed + kt * (m.k + m.k_round * rounds + m.k_load * load) + m.round * rounds +
+                     (epi == EPI_STORE ? m.load_store : epi == EPI_GELU ? m.load_gelu :
+                      epi == EPI_RESID ? m.load_resid : m.load_fp8) * load;
+    if (best < 0 || t < best_t) {
+      best = c;
+      best_t = t;
+    }
+  }
+  return best;
 }
 
 template <int EPI>
 hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
-  launch((k_gemm8_rows<EPI>), dim3((uint32_t)(((int64_t)a.N + 127) / 128 * (((int64_t)a.M + 15) / 16))), dim3(512), 0, s, a);
-  return hipGetLastError();
+  switch (choose_tiles(a.M, a.N, a.K, EPI)) {
+    case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1>(a, s);
+    case 1: return launch_dma<128, 256, 1, 4, 1, 2, EPI, 2>(a, s);
+    case 2: return launch_dma<128, 128, 2, 2, 1, 3, EPI, 16>(a, s);
+    case 3: return launch_dma<128, 128, 2, 4, 4, 2, EPI, 1>(a, s);
+    case 4: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2>(a, s);
+    case 5: return launch_dma<32, 128, 1, 4, 7, 1, EPI, 4>(a, s);
+    case 6: return launch_dma<32, 128, 1, 4, 3, 2, EPI, 4>(a, s);
+    case 7:
+      if constexpr (EPI != EPI_GELU_FP8) return launch_dma<32, 64, 1, 2, 5, 1, EPI, 4>(a, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -133,7 +588,7 @@ hipError_t launch_gemm_fp8(int epi, int M, int N, int K, const void* A, int64_t 
                            int64_t ldr, hipStream_t s) {
   if (M == 0) return hipSuccess;
   Gemm8Args a{M, N, K, (const uint8_t*)A, lda, (const uint8_t*)sa, ldsa, (const uint8_t*)W, ldw, (const uint8_t*)sw,
-              ldsw, bias, gate, out, ldo, (uint8_t*)so, ldso, resid, ldr};
+              ldsw, bias, gate, out, ldo, (uint8_t*)so, ldso, resid, ldr, 1};
   switch (epi) {
     case EPI_STORE: return launch_epi<EPI_STORE>(a, s);
     case EPI_GELU: return launch_epi<EPI_GELU>(a, s);
