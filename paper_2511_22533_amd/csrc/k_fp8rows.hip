@@ -16,13 +16,22 @@ __device__ __forceinline__ Eight load8(const float* p) {
   return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
 
-__device__ __forceinline__ Eight load8(const bf16* p) {
-  const bf16x8 a = *reinterpret_cast<const bf16x8*>(p);
+// Eight values as they are stored.
+template <typename T> struct Raw8;
+template <> struct Raw8<float> { Eight v; };
+template <> struct Raw8<bf16> { bf16x8 v; };
+
+__device__ __forceinline__ Raw8<float> raw8(const float* p) { return {load8(p)}; }
+__device__ __forceinline__ Raw8<bf16> raw8(const bf16* p) { return {*reinterpret_cast<const bf16x8*>(p)}; }
+__device__ __forceinline__ Eight widen(const Raw8<float>& a) { return a.v; }
+__device__ __forceinline__ Eight widen(const Raw8<bf16>& a) {
   Eight r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r.v[e] = (float)a[e];
+  for (int e = 0; e < 8; ++e) r.v[e] = (float)a.v[e];
   return r;
 }
+
+__device__ __forceinline__ Eight load8(const bf16* p) { return widen(raw8(p)); }
 
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -101,13 +110,18 @@ __global__ __launch_bounds__(256) void k_quant_tiles(const T* __restrict__ x, in
   if (tid == 0) scale[by * lds + bx] = (uint8_t)byte;
 }
 
-// The pass between two blocks. One wave holds a row in registers, 8 columns a
-// lane and 512 a piece: p = post(y) post_w, h += rs gate p, u = pre(h) pre_w,
-// out = u (1 + scale) + shift. Both norms take their statistics over the row in
+// The pass between two blocks: p = post(y) post_w, h += rs gate p, u = pre(h)
+// pre_w, out = u (1 + scale) + shift. WPR waves hold a row in registers, 8 columns
+// a lane and 512 or 1024 a wave; sums over a wave on DPP adds and half swaps, over
+// more waves through LDS. Both norms take their statistics over the row in
 // float32, the variance about the mean.
+//
+// A wave keeps its columns of the vectors, combined to three (rs gate post_w, pre_w
+// (1 + scale), shift), in registers over the run of rows that it works off: read
+// for each row they are up to 20 bytes a column beside the row's own 11.
 struct ResidNormArgs {
   Segs rows;
-  int d, post, pre;
+  int d, post, pre, run;                           // run: rows that a workgroup (or wave) works off
   float eps, rs;
   const void* y;
   int64_t ldy;
@@ -125,123 +139,158 @@ struct ResidNormArgs {
   int64_t lds;
 };
 
-template <int NP>
-__device__ __forceinline__ void normalise(float (&v)[NP][8], int kind, int lane, int d, float eps) {
-  if (kind == NORM_NONE) return;
-  const float inv_d = 1.0f / (float)d;
-  if (kind == NORM_LAYER) {
-    float s = 0.0f;
+template <typename TY, int OUT, int NP, int WPR>
+__global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR, WPR > 4 ? 4 : 1) void k_resid_norm(ResidNormArgs p) {
+  __shared__ float part[2][WPR];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c0 = (WPR == 1 ? 0 : wave * NP * 512) + lane * 8;
+  int turn = 0;
+  auto row_sum = [&](float v) {
+    v = wave_sum(v);
+    if constexpr (WPR > 1) {
+      // (two places in turn: whoever writes one again has passed the barrier behind
+      // which everyone has read it)
+      if (lane == 0) part[turn][wave] = v;
+      __syncthreads();
+      v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WPR; ++w) v += part[turn][w];
+      turn ^= 1;
+    }
+    return v;
+  };
+  const float inv_d = 1.0f / (float)p.d;
+  auto normalise = [&](float (&v)[NP][8], int kind) {   // returns the factor that is left to apply
+    if (kind == NORM_NONE) return 1.0f;
+    if (kind == NORM_LAYER) {
+      float s = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NP; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += v[j][e];       // (0 past the row's end)
+      const float mean = row_sum(s) * inv_d;
+#pragma unroll
+      for (int j = 0; j < NP; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[j][e] = c0 + j * 512 < p.d ? v[j][e] - mean : 0.0f;
+    }
+    float q = 0.0f;
 #pragma unroll
     for (int j = 0; j < NP; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += v[j][e];      // (0 past the row's end)
-    const float mean = wave_sum(s) * inv_d;
+      for (int e = 0; e < 8; ++e) q += v[j][e] * v[j][e];
+    return rsqrtf(row_sum(q) * inv_d + p.eps);
+  };
+  const uint32_t total = (uint32_t)(p.rows.off[p.rows.B] - p.rows.off[0]);
+  const uint32_t first = (WPR == 1 ? blockIdx.x * 4u + wave : blockIdx.x) * (uint32_t)p.run;
+  if (first >= total) return;
+  const uint32_t last = min(total - first, (uint32_t)p.run) + first;
+  int b = find_segment(p.rows.off, p.rows.B, p.rows.off[0] + (int)first), end = 0;
+  float fg[NP][8], fs[NP][8], sh[NP][8];           // rs gate post_w, pre_w (1 + scale), shift
+  // a row's loads are issued a row ahead; of six and eight waves only one workgroup
+  // would fit on a CU with the registers of that
+  constexpr bool kAhead = WPR <= 4;
+  Eight nh[NP];
+  Raw8<TY> ny[NP];
+  auto fetch = [&](int row) {
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
-      const bool in = j * 512 + lane * 8 < d;
+      const int c = c0 + j * 512;
+      nh[j] = Eight{};
+      ny[j] = Raw8<TY>{};
+      if (c < p.d) {
+        nh[j] = load8(p.h + row * p.ldh + c);
+        if (p.y) ny[j] = raw8(reinterpret_cast<const TY*>(p.y) + row * p.ldy + c);
+      }
+    }
+  };
+  if (kAhead) fetch(p.rows.off[0] + (int)first);
+  for (uint32_t i = first; i < last; ++i) {
+    const int row = p.rows.off[0] + (int)i;
+    float* hr = p.h + row * p.ldh;
+    float h[NP][8], y[NP][8];
+    if (!kAhead) fetch(row);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[j][e] = in ? v[j][e] - mean : 0.0f;
+    for (int j = 0; j < NP; ++j) {
+      const Eight t = widen(ny[j]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[j][e] = nh[j].v[e], y[j][e] = t.v[e];
+    }
+    if (kAhead && i + 1 < last) fetch(row + 1);
+    if (row >= end) {                              // the first row, or another sample's
+      while (p.rows.off[b + 1] <= row) ++b;
+      end = p.rows.off[b + 1];
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        const int c = c0 + j * 512;
+        Eight g, w, v, z, t{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g.v[e] = w.v[e] = v.v[e] = 1.0f, z.v[e] = 0.0f;
+        if (c < p.d) {
+          if (p.gate) g = load8(p.gate + b * p.ldm + c);
+          if (p.post_w) w = load8(p.post_w + c);
+          if (p.pre_w) v = load8(p.pre_w + c);
+          if (p.scale) z = load8(p.scale + b * p.ldm + c), t = load8(p.shift + b * p.ldm + c);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          fg[j][e] = p.rs * g.v[e] * w.v[e];
+          fs[j][e] = v.v[e] * (1.0f + z.v[e]);
+          sh[j][e] = t.v[e];
+        }
+      }
+    }
+    if (p.y) {
+      const float r = normalise(y, p.post);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[j][e] += y[j][e] * r * fg[j][e];
+        if (c0 + j * 512 < p.d) store8(hr + c0 + j * 512, h[j]);
+      }
+    }
+    if (!p.out) continue;
+    const float r = normalise(h, p.pre);
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      const int c = c0 + j * 512;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[j][e] = h[j][e] * r * fs[j][e] + sh[j][e];
+      if constexpr (OUT == DT_FP8) {
+        const uint32_t byte = fp8_scale_byte(row16_max(c < p.d ? amax8(h[j]) : 0.0f));
+        if (c < p.d) {
+          store8_fp8(reinterpret_cast<uint8_t*>(p.out) + row * p.ldo + c, h[j], fp8_scale(byte));
+          if ((lane & 15) == 0) p.out_scale[row * p.lds + c / kFp8Block] = (uint8_t)byte;
+        }
+      } else if (c < p.d) {
+        if constexpr (OUT == DT_BF16) store8(reinterpret_cast<bf16*>(p.out) + row * p.ldo + c, h[j]);
+        else store8(reinterpret_cast<float*>(p.out) + row * p.ldo + c, h[j]);
+      }
     }
   }
-  float q = 0.0f;
-#pragma unroll
-  for (int j = 0; j < NP; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q += v[j][e] * v[j][e];
-  const float r = rsqrtf(wave_sum(q) * inv_d + eps);
-#pragma unroll
-  for (int j = 0; j < NP; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][e] *= r;
 }
 
-template <typename TY, int OUT, int NP>
-__global__ __launch_bounds__(256) void k_resid_norm(ResidNormArgs p) {
-  const int lane = threadIdx.x & 63;
-  const uint32_t i = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (i >= (uint32_t)(p.rows.off[p.rows.B] - p.rows.off[0])) return;
-  const int row = p.rows.off[0] + (int)i;
-  const int64_t b = find_segment(p.rows.off, p.rows.B, row);
-  float* hr = p.h + row * p.ldh;
-  float h[NP][8];
-#pragma unroll
-  for (int j = 0; j < NP; ++j) {
-    const int c = j * 512 + lane * 8;
-    Eight r{};
-    if (c < p.d) r = load8(hr + c);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[j][e] = r.v[e];
-  }
-  if (p.y) {
-    const TY* yr = reinterpret_cast<const TY*>(p.y) + row * p.ldy;
-    float y[NP][8];
-#pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int c = j * 512 + lane * 8;
-      Eight r{};
-      if (c < p.d) r = load8(yr + c);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[j][e] = r.v[e];
-    }
-    normalise<NP>(y, p.post, lane, p.d, p.eps);
-#pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int c = j * 512 + lane * 8;
-      if (c >= p.d) continue;
-      if (p.post_w) {
-        const Eight w = load8(p.post_w + c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] *= w.v[e];
-      }
-      if (p.gate) {
-        const Eight g = load8(p.gate + b * p.ldm + c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] *= g.v[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) h[j][e] += p.rs * y[j][e];
-      store8(hr + c, h[j]);
-    }
-  }
-  if (!p.out) return;
-  normalise<NP>(h, p.pre, lane, p.d, p.eps);
-#pragma unroll
-  for (int j = 0; j < NP; ++j) {
-    const int c = j * 512 + lane * 8;
-    if (c < p.d) {
-      if (p.pre_w) {
-        const Eight w = load8(p.pre_w + c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[j][e] *= w.v[e];
-      }
-      if (p.scale) {
-        const Eight sc = load8(p.scale + b * p.ldm + c), sh = load8(p.shift + b * p.ldm + c);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[j][e] = h[j][e] * (1.0f + sc.v[e]) + sh.v[e];
-      }
-    }
-    if constexpr (OUT == DT_FP8) {
-      const uint32_t byte = fp8_scale_byte(row16_max(amax8(h[j])));   // (0 past the row's end)
-      if (c < p.d) {
-        store8_fp8(reinterpret_cast<uint8_t*>(p.out) + row * p.ldo + c, h[j], fp8_scale(byte));
-        if ((lane & 15) == 0) p.out_scale[row * p.lds + c / kFp8Block] = (uint8_t)byte;
-      }
-    } else if (c < p.d) {
-      if constexpr (OUT == DT_BF16) store8(reinterpret_cast<bf16*>(p.out) + row * p.ldo + c, h[j]);
-      else store8(reinterpret_cast<float*>(p.out) + row * p.ldo + c, h[j]);
-    }
-  }
+template <typename TY, int OUT, int NP, int WPR>
+hipError_t launch_resid_norm_w(ResidNormArgs a, int64_t rows, hipStream_t s) {
+  // about twice as many waves as the chip holds, the rows in equal runs
+  const int64_t workers = 8192 / WPR;
+  a.run = (int)((rows + workers - 1) / workers);
+  const int64_t used = (rows + a.run - 1) / a.run;
+  launch((k_resid_norm<TY, OUT, NP, WPR>), dim3((uint32_t)(WPR == 1 ? (used + 3) / 4 : used)),
+         dim3(WPR == 1 ? 256 : 64 * WPR), 0, s, a);
+  return hipGetLastError();
 }
 
 template <typename TY, int OUT>
 hipError_t launch_resid_norm_t(const ResidNormArgs& a, int rows, hipStream_t s) {
-  const dim3 grid(((uint32_t)rows + 3) / 4), block(256);
-  if (a.d <= 512) launch((k_resid_norm<TY, OUT, 1>), grid, block, 0, s, a);
-  else if (a.d <= 1024) launch((k_resid_norm<TY, OUT, 2>), grid, block, 0, s, a);
-  else if (a.d <= 2048) launch((k_resid_norm<TY, OUT, 4>), grid, block, 0, s, a);
-  else if (a.d <= 4096) launch((k_resid_norm<TY, OUT, 8>), grid, block, 0, s, a);
-  else launch((k_resid_norm<TY, OUT, 16>), grid, block, 0, s, a);
-  return hipGetLastError();
+  if (a.d <= 512) return launch_resid_norm_w<TY, OUT, 1, 1>(a, rows, s);
+  if (a.d <= 1024) return launch_resid_norm_w<TY, OUT, 2, 1>(a, rows, s);
+  if (a.d <= 1536) return launch_resid_norm_w<TY, OUT, 1, 3>(a, rows, s);
+  if (a.d <= 2048) return launch_resid_norm_w<TY, OUT, 2, 2>(a, rows, s);
+  if (a.d <= 3072) return launch_resid_norm_w<TY, OUT, 2, 3>(a, rows, s);
+  if (a.d <= 4096) return launch_resid_norm_w<TY, OUT, 2, 4>(a, rows, s);
+  if (a.d <= 6144) return launch_resid_norm_w<TY, OUT, 2, 6>(a, rows, s);
+  return launch_resid_norm_w<TY, OUT, 2, 8>(a, rows, s);
 }
 
 template <typename TY>
@@ -284,7 +333,7 @@ hipError_t launch_resid_norm(int dt, int out_dt, int post, int pre, float eps, f
                              int64_t ldm, void* out, int64_t ldo, void* out_scale, int64_t lds, hipStream_t s) {
   const int n = rows.off[rows.B] - rows.off[0];
   if (n == 0 || (!y && !out)) return hipSuccess;
-  ResidNormArgs a{rows, d, post, pre, eps, resid_scale, y, ldy, post_w, gate, h, ldh, pre_w, shift, scale, ldm,
+  ResidNormArgs a{rows, d, post, pre, 1, eps, resid_scale, y, ldy, post_w, gate, h, ldh, pre_w, shift, scale, ldm,
                   out, ldo, (uint8_t*)out_scale, lds};
   return dt == DT_BF16 ? launch_resid_norm_y<bf16>(a, out_dt, n, s) : launch_resid_norm_y<float>(a, out_dt, n, s);
 }

@@ -533,53 +533,64 @@ def op_ln_mod(dtype: int, h, out, shift=None, scale=None, stream=None):
 
 
 # ------------------------------------------------------------- 8-bit operators
+# Calls of a few microseconds: the checks below look at each property of a tensor
+# once, and the current stream is asked for by device index.
 
-def _rows(name: str, t, dtypes: Sequence, shape=None):
-    """t as rows for the C ABI: a 2-D tensor of one of these types with contiguous columns, on the current device."""
-    import torch
-    if t.dtype not in [getattr(torch, d) for d in dtypes]:
-        raise ValueError(f"{name}: {t.dtype}, expected {' or '.join(dtypes)}")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+_types = None
+
+
+def _dtypes():
+    """Torch types of the operators' element types and of scale bytes (torch is imported on first use)."""
+    global _types
+    if _types is None:
+        import torch
+        fp8, byte = torch.float8_e4m3fn, torch.uint8
+        _types = {F3C_F32: (torch.float32,), F3C_BF16: (torch.bfloat16,), F3C_FP8: (fp8, byte),
+                  "scale": (torch.float8_e8m0fnu, byte), "torch": torch}
+    return _types
+
+
+def _device(t, torch) -> int:
+    """Index of t's GPU, which must be the current one (a call is enqueued on its current stream)."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"tensors on the current GPU expected, got one on {t.device}")
+    return dev
+
+
+def _rows(name: str, t, types, rows: int, cols: int, dev: int):
+    """(address, row stride) of t, rows x cols of one of these types with contiguous columns. A single row's stride
+    says nothing: then its length, rounded up to 16 bytes."""
+    if t.dtype not in types or t.get_device() != dev or t.shape != (rows, cols):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {types[0]} {(rows, cols)} on "
+                         f"the current GPU")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: rows with contiguous columns expected")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: {tuple(t.shape)}, expected {tuple(shape)}")
-    return _on_device(name, t)
+    if rows < 2:
+        unit = 16 // t.element_size()
+        ld = (cols + unit - 1) // unit * unit
+    return t.data_ptr(), ld
 
 
-def _on_device(name: str, t):
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, expected the current GPU")
-    return t
+def _scale_rows(name: str, t, types, rows: int, cols: int, dev: int):
+    """The same for the scales of `cols` columns, whose rows may be longer."""
+    need = ((cols + 127) // 128 + 3) // 4 * 4
+    if t.dim() != 2 or t.shape[1] < need:
+        raise ValueError(f"{name}: {tuple(t.shape)}, expected [{rows}][{need} or more]")
+    return _rows(name, t, types, rows, t.shape[1], dev)
 
 
-def _vector(name: str, t, n: int):
-    import torch
+def _vector(name: str, t, types, n: int, dev: int):
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: {n} contiguous float32 values expected")
-    return _on_device(name, t).data_ptr()
+    if t.dtype not in types or t.get_device() != dev or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: {n} contiguous float32 values on the current GPU expected")
+    return t.data_ptr()
 
 
-def _ld(t) -> int:
-    """Row stride; of a single row (or none), whose stride says nothing, its length rounded up to 16 bytes."""
-    if t.shape[0] > 1:
-        return t.stride(0)
-    step = 16 // t.element_size()
-    return (t.shape[1] + step - 1) // step * step
-
-
-_FP8 = ("float8_e4m3fn", "uint8")
-_SCALE = ("float8_e8m0fnu", "uint8")
-_FLOAT = {F3C_F32: ("float32",), F3C_BF16: ("bfloat16",), F3C_FP8: _FP8}
-
-
-def _scale_rows(name: str, t, rows: int, cols: int):
-    _rows(name, t, _SCALE)
-    if t.shape[0] != rows or t.shape[1] < fp8_scale_stride(cols):
-        raise ValueError(f"{name}: {tuple(t.shape)}, expected [{rows}][{fp8_scale_stride(cols)} or more]")
-    return t
+def _stream_on(stream, dev: int, torch) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream)
 
 
 def fp8_scale_stride(cols: int) -> int:
@@ -589,42 +600,40 @@ def fp8_scale_stride(cols: int) -> int:
 
 def op_quant_fp8(dtype: int, x, q, scale, block_rows: int = 1, stream=None):
     """x [R][K] -> q (e4m3 [R][K]) and scale (E8M0 bytes [ceil(R / block_rows)][fp8_scale_stride(K)])."""
-    if dtype not in (F3C_F32, F3C_BF16) or block_rows not in (1, 128):
-        raise ValueError("dtype F3C_F32 or F3C_BF16, block_rows 1 or 128")
-    _rows("x", x, _FLOAT[dtype])
+    T = _dtypes()
+    if dtype not in (F3C_F32, F3C_BF16) or block_rows not in (1, 128) or x.dim() != 2:
+        raise ValueError("rows of dtype F3C_F32 or F3C_BF16 and block_rows 1 or 128 expected")
     R, K = x.shape
-    _rows("q", q, _FP8, (R, K))
-    _scale_rows("scale", scale, (R + block_rows - 1) // block_rows, K)
-    check(lib().f3c_op_quant_fp8(dtype, block_rows, R, K, x.data_ptr(), _ld(x), q.data_ptr(), _ld(q),
-                                 scale.data_ptr(), _ld(scale), _stream(stream)))
+    dev = _device(x, T["torch"])
+    check((_lib or lib()).f3c_op_quant_fp8(
+        dtype, block_rows, R, K, *_rows("x", x, T[dtype], R, K, dev), *_rows("q", q, T[F3C_FP8], R, K, dev),
+        *_scale_rows("scale", scale, T["scale"], (R + block_rows - 1) // block_rows, K, dev),
+        _stream_on(stream, dev, T["torch"])))
 
 
 def op_gemm_fp8(epilogue: int, A, A_scale, W, W_scale, bias=None, out=None, out_scale=None, resid=None, gate=None,
                 stream=None):
     """op_gemm on 8-bit operands (op_quant_fp8's: A per row, W with block_rows 128). Epilogue 3 writes GELU as 8-bit
     rows: out e4m3 and out_scale."""
-    if epilogue not in (0, 1, 2, 3):
-        raise ValueError("epilogue 0..3 expected")
-    _rows("A", A, _FP8)
-    M, K = A.shape
-    N = W.shape[0]
-    _rows("W", W, _FP8, (N, K))
-    _scale_rows("A_scale", A_scale, M, K)
-    _scale_rows("W_scale", W_scale, (N + 127) // 128, K)
+    T = _dtypes()
+    if epilogue not in (0, 1, 2, 3) or A.dim() != 2 or W.dim() != 2:
+        raise ValueError("epilogue 0..3 and rows of A and W expected")
     if epilogue == 2:
         if resid is None or out is not None or out_scale is not None:
             raise ValueError("epilogue 2 updates resid alone")
-        _rows("resid", resid, ("float32",), (M, N))
-    else:
-        if out is None or resid is not None or (out_scale is None) != (epilogue != 3):
-            raise ValueError("epilogues 0 and 1 write out, 3 out and out_scale")
-        _rows("out", out, _FP8 if epilogue == 3 else ("bfloat16",), (M, N))
-        if epilogue == 3:
-            _scale_rows("out_scale", out_scale, M, N)
-    opt = lambda t: (None, 0) if t is None else (t.data_ptr(), _ld(t))  # noqa: E731
-    check(lib().f3c_op_gemm_fp8(epilogue, M, N, K, A.data_ptr(), _ld(A), A_scale.data_ptr(), _ld(A_scale),
-                                W.data_ptr(), _ld(W), W_scale.data_ptr(), _ld(W_scale), _vector("bias", bias, N),
-                                _vector("gate", gate, N), *opt(out), *opt(out_scale), *opt(resid), _stream(stream)))
+    elif out is None or resid is not None or (out_scale is None) != (epilogue != 3):
+        raise ValueError("epilogues 0 and 1 write out, 3 out and out_scale")
+    M, K = A.shape
+    N = W.shape[0]
+    dev = _device(A, T["torch"])
+    none, f32, fp8 = (None, 0), T[F3C_F32], T[F3C_FP8]
+    check((_lib or lib()).f3c_op_gemm_fp8(
+        epilogue, M, N, K, *_rows("A", A, fp8, M, K, dev), *_scale_rows("A_scale", A_scale, T["scale"], M, K, dev),
+        *_rows("W", W, fp8, N, K, dev), *_scale_rows("W_scale", W_scale, T["scale"], (N + 127) // 128, K, dev),
+        _vector("bias", bias, f32, N, dev), _vector("gate", gate, f32, N, dev),
+        *(none if out is None else _rows("out", out, fp8 if epilogue == 3 else T[F3C_BF16], M, N, dev)),
+        *(none if out_scale is None else _scale_rows("out_scale", out_scale, T["scale"], M, N, dev)),
+        *(none if resid is None else _rows("resid", resid, f32, M, N, dev)), _stream_on(stream, dev, T["torch"])))
 
 
 def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out_scale=None, post: int = F3C_NORM_NONE,
@@ -633,35 +642,37 @@ def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out
     """The pass between two blocks: h += resid_scale * gate * (post(y) * post_w), out = (pre(h) * pre_w) * (1 + scale)
     + shift. off: row offsets of the samples (default: one sample of all rows); gate, shift, scale [B][d], or [d] for
     all samples. y None: the norm alone; out None: the update alone."""
-    if dtype not in (F3C_F32, F3C_BF16) or out_dtype not in _FLOAT:
-        raise ValueError("dtype F3C_F32 or F3C_BF16, out_dtype F3C_F32, F3C_BF16 or F3C_FP8")
-    _rows("h", h, ("float32",))
+    T = _dtypes()
+    if dtype not in (F3C_F32, F3C_BF16) or out_dtype not in (F3C_F32, F3C_BF16, F3C_FP8) or h.dim() != 2:
+        raise ValueError("rows h, dtype F3C_F32 or F3C_BF16, out_dtype F3C_F32, F3C_BF16 or F3C_FP8 expected")
     R, d = h.shape
-    off = [0, R] if off is None else [int(v) for v in off]
+    off = (0, R) if off is None else off
     B = len(off) - 1
-    if B < 1 or off[-1] > R:
+    if B < 1 or min(off) < 0 or max(off) > R:
         raise ValueError("off: B + 1 row offsets within h expected")
-    if y is not None:
-        _rows("y", y, _FLOAT[dtype], (R, d))
-    if out is not None:
-        _rows("out", out, _FLOAT[out_dtype], (R, d))
-        if (out_scale is None) != (out_dtype != F3C_FP8):
-            raise ValueError("out_scale goes with F3C_FP8 rows")
-        if out_scale is not None:
-            _scale_rows("out_scale", out_scale, R, d)
-    mods = [(n, t) for n, t in (("gate", gate), ("shift", shift), ("scale", scale)) if t is not None]
-    ldm = None
-    for name, t in mods:
+    if (out_scale is None) == (out is not None and out_dtype == F3C_FP8):
+        raise ValueError("out_scale goes with F3C_FP8 rows")
+    dev = _device(h, T["torch"])
+    none, f32 = (None, 0), T[F3C_F32]
+    mods, ldm = [], None
+    for name, t in (("gate", gate), ("shift", shift), ("scale", scale)):
+        if t is None:
+            mods.append(None)
+            continue
         if t.dim() == 1:
-            _vector(name, t, d)
+            ptr, ld = _vector(name, t, f32, d, dev), 0
         else:
-            _rows(name, t, ("float32",), (B, d))
-        ld = 0 if t.dim() == 1 or B == 1 else t.stride(0)
+            ptr, ld = _rows(name, t, f32, B, d, dev)
+            ld = 0 if B == 1 else ld
         if ldm is not None and ld != ldm:
             raise ValueError("gate, shift and scale must have one row stride")
+        mods.append(ptr)
         ldm = ld
     c = ResidNormCfg(dtype, out_dtype, post, pre, eps, resid_scale)
-    opt = lambda t: (None, 0) if t is None else (t.data_ptr(), _ld(t))  # noqa: E731
-    check(lib().f3c_op_resid_norm(ctypes.byref(c), d, B, _i32(off), *opt(y), _vector("post_w", post_w, d), _ptr(gate),
-                                  h.data_ptr(), _ld(h), _vector("pre_w", pre_w, d), _ptr(shift), _ptr(scale),
-                                  ldm or 0, *opt(out), *opt(out_scale), _stream(stream)))
+    check((_lib or lib()).f3c_op_resid_norm(
+        ctypes.byref(c), d, B, (c_int * (B + 1))(*off), *(none if y is None else _rows("y", y, T[dtype], R, d, dev)),
+        _vector("post_w", post_w, f32, d, dev), mods[0], *_rows("h", h, f32, R, d, dev),
+        _vector("pre_w", pre_w, f32, d, dev), mods[1], mods[2], ldm or 0,
+        *(none if out is None else _rows("out", out, T[out_dtype], R, d, dev)),
+        *(none if out_scale is None else _scale_rows("out_scale", out_scale, T["scale"], R, d, dev)),
+        _stream_on(stream, dev, T["torch"])))
