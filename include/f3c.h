@@ -401,9 +401,9 @@ int f3c_op_ln_mod(int32_t dtype, int32_t rows, int32_t d, const float* h, const 
  * block is the smallest 2^e, e in [-126, 127], with |x| <= 448 * 2^e for all its
  * finite x (2^-126 if there is none but zeros); q = x * 2^-e, an exact product,
  * rounded to nearest even. NaN and infinities become NaN and do not count for
- * the scale. K a multiple of 8; x and q rows 16- and 8-byte aligned. Errors:
- * F3C_EINVAL (dtype, block_rows, shape, leading dims, NULL or misaligned
- * pointers). */
+ * the scale. K a multiple of 8; x and q rows 16- and 8-byte aligned; fewer than
+ * 2^28 blocks of 1 x 128 or 2^24 of 128 x 128. Errors: F3C_EINVAL (dtype,
+ * block_rows, shape, leading dims, NULL or misaligned pointers). */
 int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K, const void* x, int32_t ldx, void* q,
                      int32_t ldq, void* scale, int32_t lds, f3c_stream stream);
 

@@ -1087,6 +1087,8 @@ int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K,
   if (ldx < K || ldq < K || !aligned_rows(x, ldx, dtype == F3C_BF16 ? 2 : 4, 16) || !aligned_rows(q, ldq, 1, 8))
     return fail(F3C_EINVAL, "bad leading dims or alignment (x rows 16 bytes, q rows 8)");
   if (int rc = check_scales("scale", scale, lds, K, rows)) return rc;
+  const int64_t blocks = ((int64_t)rows + block_rows - 1) / block_rows * (((int64_t)K + 127) / 128);
+  if (blocks >= (block_rows == 1 ? 1 << 28 : 1 << 24)) return fail(F3C_EINVAL, "too many blocks for one launch");
   HIP_TRY(launch_quant_fp8(dtype, block_rows, rows, K, x, ldx, q, ldq, scale, lds, (hipStream_t)stream));
   return F3C_OK;
 }

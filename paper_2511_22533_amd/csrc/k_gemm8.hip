@@ -15,6 +15,7 @@
 // bit); the bf16 ones do, at half the rate.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "fp8.h"
 #include "kernels.h"
@@ -419,16 +420,16 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
       open(kt + 1);
     }
   } else {
-  // After the barrier that frees tile kt's stage (behind product TN - 1 of its
-  // second K-step), tile kt + STAGES goes into it: over the rest of that K-step,
-  // and with more than two stages over the next one as well.
-  constexpr int SLOTS = GS - TN + 1 + (STAGES > 2 ? GS : 0), FAST = (DT + DPI - 1) / DPI < SLOTS ? (DT + DPI - 1) / DPI : SLOTS;
+  // Behind the barrier that frees tile kt's stage (before product TN of its second
+  // K-step), tile kt + STAGES goes into it: over the rest of that K-step, and with
+  // more than two stages over the next one as well.
+  constexpr int HEAD = GS > TN ? GS - TN : 1, SLOTS = HEAD + (STAGES > 2 ? GS : 0), FAST = (DT + DPI - 1) / DPI < SLOTS ? (DT + DPI - 1) / DPI : SLOTS;
   auto slot = [](int q) { return q * FAST / DT; };
   auto wpos = [](int f, int from) { return from + f * (GS - from) / TN; };
   int stage = 0, dstage = STAGES - 1, dt = min(STAGES - 1, KT - 1);
   constexpr int EARLY = [] {                       // a tile's instructions within its first K-step's slots
     int n = 0;
-    for (int q = 0; q < DT; ++q) n += q * FAST / DT < GS - TN + 1;
+    for (int q = 0; q < DT; ++q) n += q * FAST / DT < HEAD;
     return n;
   }();
 #pragma unroll
@@ -443,59 +444,81 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   // (in the loop's order, so that the compiler's waits in it are exact)
   read_scales(0);
 #pragma unroll
-  for (int n = TN - 1; n < GS; ++n) {
-    if (n % TN == TN - 1) read_a(n / TN, 0);
+  for (int n = TN; n < GS + TN; ++n) {
+    if (n == TN) read_a(0, 0);
+    if (n < GS && n % TN == TN - 1) read_a(n / TN, 0);
 #pragma unroll
     for (int f = 0; f < TN; ++f)
-      if (n == wpos(f, TN - 1)) read_w(f, 0);
+      if (n == (GS > TN ? wpos(f, TN) : TN)) read_w(f, 0);
     fence();
   }
   take_scales(0);
   fence();
-  for (int kt = 0; kt < KT; ++kt) {
+  // Products n0..n1 of K-step ks, the next K-step's fragment reads (next) and the
+  // DMA (slots counted from the barrier) among them.
+  auto products = [&](auto ks_, auto from_, auto to_, bool next) {
+    constexpr int ks = decltype(ks_)::value, from = decltype(from_)::value, to = decltype(to_)::value;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int n = from; n < to; ++n) {
+      const int i = n / TN, j = n % TN, nxt = ks ^ 1;
+      product(ks, i, j);
+      if (next) {
+        // (behind the barrier the fragment of row block 0 is free already)
+        if (ks == 1 && n == TN) read_a(0, nxt);
+        if (j == TN - 1) read_a(i, nxt);
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int f = 0; f < TN; ++f)
+          if (n == wpos(f, ks == 1 ? TN : 0)) read_w(f, nxt);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int n = i * TN + j, nxt = ks ^ 1;
-          product(ks, i, j);
-          if (ks == 1 && n == TN - 1) {
-            // every wave holds this tile's last fragments and tile kt + 1 has
-            // landed: one barrier retires tile kt's stage and opens kt + 1's
-            __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
-            wait_vm<(STAGES - 2) * DT>();
-            __builtin_amdgcn_s_barrier();
-            fence();
-            dstage = stage;
-            dt = min(kt + STAGES, KT - 1);
-            cut_tail(kt + STAGES);
-            const uint32_t d = stage == STAGES - 1 ? (uint32_t)(-(STAGES - 1) * SBUF) : (uint32_t)SBUF;
-            stage = stage == STAGES - 1 ? 0 : stage + 1;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                aad[k][x] += d;
-                wad[k][x] += d;
-              }
-            read_scales(stage);
-            fence();
-          }
-          if (j == TN - 1) read_a(i, nxt);
-          // the next K-step's weights: from this one's start, or from the barrier on
-#pragma unroll
-          for (int f = 0; f < TN; ++f)
-            if (n == wpos(f, ks == 1 ? TN - 1 : 0)) read_w(f, nxt);
-#pragma unroll
-          for (int q = 0; q < DT; ++q)
-            if (slot(q) == (ks == 1 ? n - (TN - 1) : n + GS - TN + 1) && (ks == 1 || STAGES > 2)) fetch1(q, dt, dstage);
-          fence();
-        }
-      if (ks == 1) take_scales(kt + 1);
+        for (int q = 0; q < DT; ++q)
+          if (slot(q) == (ks == 1 ? n - TN : n + HEAD) && (ks == 1 || STAGES > 2)) fetch1(q, dt, dstage);
+      }
+      fence();
     }
+  };
+  constexpr std::integral_constant<int, 0> c0{};
+  constexpr std::integral_constant<int, 1> c1{};
+  constexpr std::integral_constant<int, TN> ctn{};
+  constexpr std::integral_constant<int, GS> cgs{};
+  products(c0, c0, cgs, true);
+  products(c1, c0, ctn, false);
+  for (int kt = 0; kt + 1 < KT; ++kt) {
+    // Every wave holds tile kt's last fragments and tile kt + 1 has landed: one
+    // barrier retires tile kt's stage and opens kt + 1's. The loop turns here, where
+    // all reads are waited for anyway (at its other places the compiler would wait
+    // for the reads just issued).
+    __builtin_amdgcn_s_waitcnt(0xc07f);            // lgkmcnt(0)
+    wait_vm<(STAGES - 2) * DT>();
+    __builtin_amdgcn_s_barrier();
+    fence();
+    dstage = stage;
+    dt = min(kt + STAGES, KT - 1);
+    cut_tail(kt + STAGES);
+    const uint32_t d = stage == STAGES - 1 ? (uint32_t)(-(STAGES - 1) * SBUF) : (uint32_t)SBUF;
+    stage = stage == STAGES - 1 ? 0 : stage + 1;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        aad[k][x] += d;
+        wad[k][x] += d;
+      }
+    read_scales(stage);
+    fence();
+    if (GS == TN) {                                // (no product is left of this K-step)
+      read_a(0, 0);
+#pragma unroll
+      for (int f = 0; f < TN; ++f) read_w(f, 0);
+#pragma unroll
+      for (int q = 0; q < DT; ++q)
+        if (slot(q) == 0) fetch1(q, dt, dstage);
+    }
+    products(c1, ctn, cgs, true);
+    take_scales(kt + 1);
+    products(c0, c0, cgs, true);
+    products(c1, c0, ctn, false);
   }
+  products(c1, ctn, cgs, false);
   }
   wait_vm<0>();
   __syncthreads();                                 // no DMA in flight, every wave past its last fragment read

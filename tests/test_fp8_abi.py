@@ -36,7 +36,8 @@ def _norm(cfg=None, off=(0, 4), null_cfg=False, **kw):
 @pytest.mark.parametrize("kw", [dict(dtype=2), dict(dtype=-1), dict(block_rows=2), dict(block_rows=0), dict(rows=-1),
                                 dict(K=0), dict(K=100), dict(x=None), dict(q=None), dict(scale=None), dict(ldx=248),
                                 dict(ldx=257), dict(ldq=250), dict(ldq=260), dict(x=P + 8), dict(q=P + 4),
-                                dict(scale=P + 1), dict(lds=1), dict(lds=6), dict(K=520, ldx=520, ldq=520, lds=4)])
+                                dict(scale=P + 1), dict(lds=1), dict(lds=6), dict(K=520, ldx=520, ldq=520, lds=4),
+                                dict(rows=1 << 28, K=128), dict(rows=(1 << 31) - 1, K=264, ldx=264, ldq=264, block_rows=128)])
 def test_quant_refuses(kw):
     assert _quant(**kw) == f3c.F3C_EINVAL
     assert f3c.lib().f3c_last_error()
