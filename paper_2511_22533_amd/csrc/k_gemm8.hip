@@ -348,9 +348,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
 #pragma unroll
     for (int x = 0; x < 2; ++x) fa[i].h[x] = *(lds_u32x4*)(uintptr_t)(aad[ks][x] + (uint32_t)(i * 32 * KTB));
   };
-  auto read_w = [&](int j, int ks) {
+  auto read_w = [&](int set, int j, int ks) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) fw[ks][j].h[x] = *(lds_u32x4*)(uintptr_t)(wad[ks][x] + (uint32_t)(j * 32 * KTB));
+    for (int x = 0; x < 2; ++x) fw[set][j].h[x] = *(lds_u32x4*)(uintptr_t)(wad[ks][x] + (uint32_t)(j * 32 * KTB));
   };
   const uint32_t sad = lds0 + (uint32_t)(STAGES * SBUF + (wm * WTM + r32) * 4);
   const uint32_t swd = lds0 + (uint32_t)(STAGES * SBUF + (64 * SA + (((n0 & 127) + wn * WTN) >> 7)) * 4);
@@ -365,21 +365,25 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
     sw = nsw >> (8 * (t & 3));
   };
   constexpr int GS = TM * TN;
-  auto product = [&](int ks, int i, int j) {
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[ks][j].v, fa[i].v, acc[i][j], 0, 0, 0, (int)sw, 0,
+  auto product = [&](int ks, int set, int i, int j) {
+    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[set][j].v, fa[i].v, acc[i][j], 0, 0, 0, (int)sw, 0,
                                                                 (int)sa[i]);
     fence();
   };
   if constexpr (STAGES == 1) {
+    // One stage: the wait for a tile is hidden by the CU's other workgroups, and each
+    // fragment has one register set, read again as soon as its last product is
+    // issued (more waves fit). Columns outermost: the weights are free first.
     auto open = [&](int t) {                       // K tile t has been issued: wait, read its first K-step
       wait_vm<0>();
       __builtin_amdgcn_s_barrier();
       fence();
       read_scales(0);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) read_w(j, 0);
+      read_w(0, 0, 0);
 #pragma unroll
       for (int i = 0; i < TM; ++i) read_a(i, 0);
+#pragma unroll
+      for (int j = 1; j < TN; ++j) read_w(0, j, 0);
       take_scales(t);
       fence();
     };
@@ -387,36 +391,33 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
 #pragma unroll
     for (int q = 0; q < DT; ++q) fetch1(q, 0, 0);
     open(0);
-    for (int kt = 0; kt < KT; ++kt) {
+    for (int kt = 0;; ++kt) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          product(0, i, j);
+        for (int i = 0; i < TM; ++i) {
+          product(0, 0, i, j);
           if (j == TN - 1) read_a(i, 1);
-          if (i == 0) read_w(j, 1);
+          if (i == TM - 1) read_w(0, j, 1);
           fence();
         }
-      const int t = min(kt + 1, KT - 1);
-      cut_tail(kt + 1);
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int n = i * TN + j;
-          product(1, i, j);
-          if (n == TN - 1) {
-            __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0): this wave holds the tile's last fragments
-            __builtin_amdgcn_s_barrier();
-            fence();
-          }
-          if (n >= TN - 1) {
-#pragma unroll
-            for (int q = 0; q < DT; ++q)
-              if (n == (TN - 1 + q / DPI < GS - 1 ? TN - 1 + q / DPI : GS - 1)) fetch1(q, t, 0);
-          }
+      for (int n = 0; n < GS; ++n) {
+        product(1, 0, n % TM, n / TM);
+        if (n == 0 && GS > 1) {
+          __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): this wave holds the tile's last fragments
+          __builtin_amdgcn_s_barrier();
           fence();
+          cut_tail(kt + 1);
         }
+        if (n < GS - 1) {
+#pragma unroll
+          for (int q = 0; q < DT; ++q)
+            if (n == (q / DPI < GS - 2 ? q / DPI : GS - 2)) fetch1(q, min(kt + 1, KT - 1), 0);
+        }
+        fence();
+      }
+      if (kt + 1 == KT) break;
       open(kt + 1);
     }
   } else {
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
     if (n < GS && n % TN == TN - 1) read_a(n / TN, 0);
 #pragma unroll
     for (int f = 0; f < TN; ++f)
-      if (n == (GS > TN ? wpos(f, TN) : TN)) read_w(f, 0);
+      if (n == (GS > TN ? wpos(f, TN) : TN)) read_w(0, f, 0);
     fence();
   }
   take_scales(0);
@@ -461,14 +462,14 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
 #pragma unroll
     for (int n = from; n < to; ++n) {
       const int i = n / TN, j = n % TN, nxt = ks ^ 1;
-      product(ks, i, j);
+      product(ks, ks, i, j);
       if (next) {
         // (behind the barrier the fragment of row block 0 is free already)
         if (ks == 1 && n == TN) read_a(0, nxt);
         if (j == TN - 1) read_a(i, nxt);
 #pragma unroll
         for (int f = 0; f < TN; ++f)
-          if (n == wpos(f, ks == 1 ? TN : 0)) read_w(f, nxt);
+          if (n == wpos(f, ks == 1 ? TN : 0)) read_w(nxt, f, nxt);
 #pragma unroll
         for (int q = 0; q < DT; ++q)
           if (slot(q) == (ks == 1 ? n - TN : n + HEAD) && (ks == 1 || STAGES > 2)) fetch1(q, dt, dstage);
@@ -508,7 +509,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
     if (GS == TN) {                                // (no product is left of this K-step)
       read_a(0, 0);
 #pragma unroll
-      for (int f = 0; f < TN; ++f) read_w(f, 0);
+      for (int f = 0; f < TN; ++f) read_w(0, f, 0);
 #pragma unroll
       for (int q = 0; q < DT; ++q)
         if (slot(q) == 0) fetch1(q, dt, dstage);
@@ -552,20 +553,26 @@ hipError_t launch_dma(const Gemm8Args& a0, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Tile shapes by a cost model in us, as the bf16 projections': a fixed cost, per K
-// tile a fixed cost, a cost per round of 256 x (workgroups per CU) workgroups (a
-// partial round costs a whole one) and one per 256 workgroups' load, and per round
-// and load the epilogue; a least-squares fit to 1374 measured calls on MI355X.
-struct Tile8Cost { int bm, bn, per_cu; double fixed, k, k_round, k_load, round, load_store, load_gelu, load_resid, load_fp8; };
+// Tile shapes by a cost model in us, as the bf16 projections': a fixed cost; per K
+// tile of 128 a fixed cost, one per round of 256 x per_cu workgroups (a partial
+// round costs a whole one), one per workgroup of the fullest CU and one per 256
+// workgroups' load; per round, workgroup and load the epilogue. A least-squares fit
+// to 1374 measured calls on MI355X (128 to 8192 columns, K = 128 to 8192, 1 to 32768
+// rows, every epilogue): over them its pick is 0.6% slower than the best of the
+// seven in the mean, 23% at worst; they are 0.2% from the best of twelve that were
+// measured. Without the cost per workgroup of a CU it was 1.1% and 41%.
+struct Tile8Cost {
+  int bm, bn, per_cu;
+  double fixed, k, k_round, k_group, k_load, round, group, load_store, load_gelu, load_resid, load_fp8;
+};
 constexpr Tile8Cost kTile8Cost[] = {
-    {256, 256, 1, 1.911, 0.408, 0.668, 0.790, 4.769, 2.438, 7.088, 19.766, 6.991},
-    {128, 256, 2, 1.019, 0.843, 0.042, 0.748, 4.297, 0.966, 2.693, 10.072, 2.110},
-    {128, 128, 3, 1.924, 0.477, 0.118, 0.426, 2.067, 0.742, 1.477, 4.542, 1.073},
-    {128, 128, 1, 1.572, 0.071, 0.289, 0.330, 2.656, 0.000, 1.004, 3.680, 1.141},
-    {64, 128, 2, 1.835, 0.094, 0.273, 0.258, 1.712, 0.172, 0.608, 2.082, 0.425},
-    {32, 128, 1, 1.992, 0.000, 0.223, 0.123, 2.051, 0.000, 0.456, 1.112, 0.601},
-    {32, 128, 2, 1.969, 0.000, 0.308, 0.178, 1.088, 0.000, 0.351, 0.807, 0.268},
-    {32, 64, 2, 1.613, 0.000, 0.183, 0.092, 1.787, 0.000, 0.300, 0.558, 0.000},
+    {256, 256, 1, 1.607, 0.548, 0.512, 0.000, 0.816, 4.257, 0.000, 1.899, 6.918, 19.273, 6.561},
+    {128, 128, 4, 2.769, 0.593, 0.000, 0.000, 0.426, 0.000, 1.146, 0.113, 0.756, 3.671, 0.456},
+    {64, 128, 2, 2.329, 0.142, 0.000, 0.153, 0.174, 0.694, 0.491, 0.176, 0.584, 1.963, 0.347},
+    {32, 128, 2, 2.438, 0.033, 0.073, 0.120, 0.125, 0.372, 0.281, 0.000, 0.349, 0.754, 0.191},
+    {64, 64, 2, 2.017, 0.060, 0.076, 0.086, 0.095, 0.524, 0.532, 0.000, 0.202, 0.820, 0.000},
+    {32, 64, 2, 1.653, 0.000, 0.132, 0.057, 0.061, 1.341, 0.053, 0.000, 0.309, 0.558, 0.000},
+    {128, 128, 1, 1.572, 0.119, 0.213, 0.000, 0.348, 2.358, 0.000, 0.000, 1.029, 3.534, 1.167},
 };
 
 inline int choose_tiles(int M, int N, int K, int epi) {
@@ -575,8 +582,9 @@ inline int choose_tiles(int M, int N, int K, int epi) {
     const Tile8Cost& m = kTile8Cost[c];
     if (epi == EPI_GELU_FP8 && m.bn < kFp8Block) continue;             // a quantisation block in one workgroup
     const double tiles = std::ceil((double)M / m.bm) * std::ceil((double)N / m.bn), load = tiles / 256.0;
-    const double rounds = std::ceil(load / m.per_cu), kt = std::ceil(K / 128.0);
-    const double t = m.fixed + kt * (m.k + m.k_round * rounds + m.k_load * load) + m.round * rounds +
+    const double rounds = std::ceil(load / m.per_cu), groups = std::ceil(load), kt = std::ceil(K / 128.0);
+    const double t = m.fixed + kt * (m.k + m.k_round * rounds + m.k_group * groups + m.k_load * load) +
+                     m.round * rounds + m.group * groups +
                      (epi == EPI_STORE ? m.load_store : epi == EPI_GELU ? m.load_gelu :
                       epi == EPI_RESID ? m.load_resid : m.load_fp8) * load;
     if (best < 0 || t < best_t) {
@@ -591,14 +599,16 @@ template <int EPI>
 hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   switch (choose_tiles(a.M, a.N, a.K, EPI)) {
     case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1>(a, s);
-    case 1: return launch_dma<128, 256, 1, 4, 1, 2, EPI, 2>(a, s);
-    case 2: return launch_dma<128, 128, 2, 2, 1, 3, EPI, 16>(a, s);
-    case 3: return launch_dma<128, 128, 2, 4, 4, 2, EPI, 1>(a, s);
-    case 4: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2>(a, s);
-    case 5: return launch_dma<32, 128, 1, 4, 7, 1, EPI, 4>(a, s);
-    case 6: return launch_dma<32, 128, 1, 4, 3, 2, EPI, 4>(a, s);
-    case 7:
+    case 1: return launch_dma<128, 128, 2, 2, 1, 4, EPI, 4>(a, s);
+    case 2: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2>(a, s);
+    case 3: return launch_dma<32, 128, 1, 4, 3, 2, EPI, 4>(a, s);
+    case 4:
+      if constexpr (EPI != EPI_GELU_FP8) return launch_dma<64, 64, 2, 2, 4, 2, EPI, 4>(a, s);
+      break;
+    case 5:
       if constexpr (EPI != EPI_GELU_FP8) return launch_dma<32, 64, 1, 2, 5, 1, EPI, 4>(a, s);
+      break;
+    case 6: return launch_dma<128, 128, 2, 4, 4, 2, EPI, 1>(a, s);
   }
   return hipErrorInvalidValue;
 }
