@@ -412,10 +412,11 @@ int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K,
  * epilogue 0: out bf16 [M][ldo] = v; 1: out bf16 = GELU_tanh(v); 2: resid f32
  * [M][ldr] += (gate ? gate[n] : 1) * v; 3: out e4m3 [M][ldo] and out_scale
  * [M][ldso] = GELU_tanh(v) quantised per 1 x 128 as f3c_op_quant_fp8 does (from
- * float32, no rounding in between). Accumulators are float32; the matrix core
- * adds the products of 8 consecutive k after aligning them to their largest and
- * drops bits 2^14 below it, so a sum of n normally distributed products is about
- * 1.3e-5 of its size off. N and K multiples of 16; rows of A, W, out and resid
+ * float32, no rounding in between). Accumulators are float32 and start from the
+ * bias; the matrix core adds the products of 8 consecutive k after aligning them
+ * to their largest and drops what lies 2^14 below it, so that v is off by 1.3e-5
+ * of its size where the operands are normally distributed and by 2e-5 where A
+ * holds GELU's outputs. N and K multiples of 16, M and N below 2^30; rows of A, W, out and resid
  * 16-byte aligned, of bias and gate too; lda, ldw, ldsa, ldsw below 2^22. The result of an
  * output row does not depend on M or on other rows, nor on scheduling. out,
  * out_scale and resid must not overlap the operands. Errors: F3C_EINVAL. */

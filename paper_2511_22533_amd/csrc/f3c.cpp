@@ -1098,7 +1098,7 @@ int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const voi
                     const float* bias, const float* gate, void* out, int32_t ldo, void* out_scale, int32_t ldso,
                     float* resid, int32_t ldr, f3c_stream stream) {
   if (epilogue < EPI_STORE || epilogue > EPI_GELU_FP8) return fail(F3C_EINVAL, "bad epilogue");
-  if (M < 0 || N <= 0 || K <= 0) return fail(F3C_EINVAL, "bad shape");
+  if (M < 0 || N <= 0 || K <= 0 || M >= (1 << 30) || N >= (1 << 30)) return fail(F3C_EINVAL, "bad shape");
   if (N % 16 || K % 16) return fail(F3C_EINVAL, "N and K must be multiples of 16");
   if ((M && !A) || !W) return fail(F3C_EINVAL, "NULL operand");
   if (lda < K || ldw < K || !aligned_rows(A, lda, 1, 16) || !aligned_rows(W, ldw, 1, 16))

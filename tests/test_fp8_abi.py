@@ -43,7 +43,7 @@ def test_quant_refuses(kw):
     assert f3c.lib().f3c_last_error()
 
 
-@pytest.mark.parametrize("kw", [dict(epi=-1), dict(epi=4), dict(M=-1), dict(N=0), dict(K=0), dict(N=250), dict(K=264),
+@pytest.mark.parametrize("kw", [dict(epi=-1), dict(epi=4), dict(M=-1), dict(M=1 << 30), dict(N=0), dict(K=0), dict(N=250), dict(K=264),
                                 dict(A=None), dict(W=None), dict(sa=None), dict(sw=None), dict(lda=240), dict(ldw=240),
                                 dict(lda=264), dict(ldw=264), dict(lda=1 << 22), dict(ldw=1 << 22), dict(A=P + 8),
                                 dict(W=P + 4), dict(sa=P + 2), dict(sw=P + 2), dict(ldsa=1), dict(ldsw=5),
