@@ -248,9 +248,9 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
   }
 }
 
-// Many rows: K tiles of 128 bytes (one scale block) go HBM -> LDS by DMA into
-// STAGES stages; each wave multiplies TM x TN tiles of 32 x 32 on 32x32x64
-// instructions, two K-steps per tile.
+// K tiles of 128 bytes (one scale block) go HBM -> LDS by DMA into STAGES stages;
+// each wave multiplies TM x TN tiles of 32 x 32 on 32x32x64 instructions, two
+// K-steps per tile.
 //
 // The weight fragment is the instruction's A operand and the activation fragment
 // its B operand (a tile of C^T), as in the bf16 kernels. A lane feeds 32 bytes of
@@ -262,17 +262,33 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // read a K-step ahead into a second set.
 //
 // Scales come with their K tile: the dword of each row that holds the tile's byte,
-// by DMA too, shifted into place as it is read. The loop over K has no branch: the
-// compiler would move products across it, out of their places between the reads.
+// by DMA too, shifted into place as it is read. The loop over K tiles has no
+// branch: the compiler would move products across it, out of their places
+// between the reads.
+//
+// What bounds it. Long K, many rows: power. On such operands the matrix cores alone,
+// from registers, sustain 3.5 to 3.8 PFLOP/s (4.9 on zeros); 8192 x 8192 x 8192 takes
+// 410 to 470 us by box (2.7 to 2.35 PFLOP/s) at a clock of 1.6 GHz with the matrix
+// pipes busy 69% of the cycles. 256 x 256 tiles read LDS least (16-byte K halves of a
+// row as stages cost 10%: lines travel twice). Short K: the epilogue beside it, mostly
+// GELU's exponential and reciprocal, which only another workgroup's products can hide:
+// at 32768 x 4096 x 1024 into 8 bits one 256 x 256 workgroup per CU takes 175 us, four
+// of 128 x 128 in a single stage 157. Into a residual it is its 268 MB. Few rows: the
+// chain of K tiles, 0.2 to 0.3 us each, of LDS reads and two dependent products.
+// Against the bf16 projections on one box (us, bf16 / here): 32768 x 4096 x 1024 GELU
+// 283 / 154 (out in 8 bits), 32768 x 1024 x 4096 residual 264 / 147, 9831 x 2048 x 1024
+// 52 / 28, 9831 x 1024 x 4096 residual 88 / 57, 820 x 1024 x 4096 residual 19 / 12.6.
 template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, bool WIDE = false>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
   constexpr int KTB = 128, ABUF = BM * KTB, SBUF = (BM + BN) * KTB;
   constexpr int DA = BM / 8, DB = BN / 8, DQ = (DA + DB) / NW;         // DMA blocks of 8 rows
-  constexpr int SA = (BM + 63) / 64, SX = (SA + NW) / NW, DT = DQ + SX;       // scale DMAs: of A, and per wave; all of a wave
+  constexpr int SA = (BM + 63) / 64, SX = (SA + NW) / NW;              // scale DMAs of A; all, per wave
+  constexpr int DT = DQ + SX;                                          // a wave's DMA instructions per K tile
   constexpr int SSET = 64 * NW * SX * 4;                               // bytes of a stage's scales
   static_assert(DA % NW == 0 && DB % NW == 0, "whole DMA blocks per wave");
   static_assert(BM % (32 * WGM) == 0 && BN % (32 * WGN) == 0 && WTN <= 128 && NW % 2 == 0, "tile shape");
+  static_assert(STAGES > 1 || TM * TN > 2, "a single stage is refilled between the products of a K-step");
   constexpr int EB = EPI == EPI_GELU_FP8 ? NW * 32 * (WTN + 16) + WGN * BM * 4 : NW * 32 * (WTN * 4 + 16);
   constexpr int LDSB = STAGES * (SBUF + SSET) > EB ? STAGES * (SBUF + SSET) : EB;
   __shared__ __attribute__((aligned(16))) char lds[LDSB];
@@ -345,7 +361,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
       }
     } else {
       const int y = q - DQ;
-      const uint32_t dst = lds0 + (uint32_t)(STAGES * SBUF + stage * SSET + (wave + NW * y) * 256), ks = (uint32_t)(t & ~3);
+      const uint32_t dst = lds0 + (uint32_t)(STAGES * SBUF + stage * SSET + (wave + NW * y) * 256);
+      const uint32_t ks = (uint32_t)(t & ~3);
       asm volatile("buffer_load_dword %0, %1, %2 offen lds"
                    : : "v"(sofs[y]), "s"(sdesc[y]), "s"(ks), "{m0}"(dst) : "memory");
     }
@@ -471,7 +488,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   // Behind the barrier that frees tile kt's stage (before product TN of its second
   // K-step), tile kt + STAGES goes into it: over the rest of that K-step, and with
   // more than two stages over the next one as well.
-  constexpr int HEAD = GS > TN ? GS - TN : 1, SLOTS = HEAD + (STAGES > 2 ? GS : 0), FAST = (DT + DPI - 1) / DPI < SLOTS ? (DT + DPI - 1) / DPI : SLOTS;
+  constexpr int HEAD = GS > TN ? GS - TN : 1, SLOTS = HEAD + (STAGES > 2 ? GS : 0);
+  constexpr int FAST = (DT + DPI - 1) / DPI < SLOTS ? (DT + DPI - 1) / DPI : SLOTS;
   auto slot = [](int q) { return q * FAST / DT; };
   auto wpos = [](int f, int from) { return from + f * (GS - from) / TN; };
   int stage = 0, dstage = STAGES - 1, dt = min(STAGES - 1, KT - 1);
@@ -596,8 +614,8 @@ hipError_t launch_dma(const Gemm8Args& a0, hipStream_t s) {
   Gemm8Args a = a0;
   a.xq = choose_xq(a.M, a.N, a.K, BM, BN);
   const int64_t tiles = (int64_t)((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM);
-  launch((k_gemm8_dma<BM, BN, WGM, WGN, STAGES, OCC, EPI, DPI, WIDE>), dim3((uint32_t)tiles), dim3(64 * WGM * WGN), 0, s,
-         a);
+  launch((k_gemm8_dma<BM, BN, WGM, WGN, STAGES, OCC, EPI, DPI, WIDE>), dim3((uint32_t)tiles), dim3(64 * WGM * WGN), 0,
+         s, a);
   return hipGetLastError();
 }
 

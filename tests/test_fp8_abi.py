@@ -37,13 +37,15 @@ def _norm(cfg=None, off=(0, 4), null_cfg=False, **kw):
                                 dict(K=0), dict(K=100), dict(x=None), dict(q=None), dict(scale=None), dict(ldx=248),
                                 dict(ldx=257), dict(ldq=250), dict(ldq=260), dict(x=P + 8), dict(q=P + 4),
                                 dict(scale=P + 1), dict(lds=1), dict(lds=6), dict(K=520, ldx=520, ldq=520, lds=4),
-                                dict(rows=1 << 28, K=128), dict(rows=(1 << 31) - 1, K=264, ldx=264, ldq=264, block_rows=128)])
+                                dict(rows=1 << 28, K=128),
+                                dict(rows=(1 << 31) - 1, K=264, ldx=264, ldq=264, block_rows=128)])
 def test_quant_refuses(kw):
     assert _quant(**kw) == f3c.F3C_EINVAL
     assert f3c.lib().f3c_last_error()
 
 
-@pytest.mark.parametrize("kw", [dict(epi=-1), dict(epi=4), dict(M=-1), dict(M=1 << 30), dict(N=0), dict(K=0), dict(N=250), dict(K=264),
+@pytest.mark.parametrize("kw", [dict(epi=-1), dict(epi=4), dict(M=-1), dict(M=1 << 30), dict(N=0), dict(K=0), dict(N=250),
+                                dict(K=264),
                                 dict(A=None), dict(W=None), dict(sa=None), dict(sw=None), dict(lda=240), dict(ldw=240),
                                 dict(lda=264), dict(ldw=264), dict(lda=1 << 22), dict(ldw=1 << 22), dict(A=P + 8),
                                 dict(W=P + 4), dict(sa=P + 2), dict(sw=P + 2), dict(ldsa=1), dict(ldsw=5),
