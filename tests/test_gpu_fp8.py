@@ -524,3 +524,160 @@ def test_graph_replays_and_streams(torch, f3c):
         b.run()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(outs(b), want_b))
+
+
+# ------------------------------------------------------------------------------------------------------- far corners
+
+def test_gemm_infinities_before_the_quantising_epilogue(torch, f3c):
+    """An infinite sum becomes NaN and does not count for its block's scale."""
+    for M, N, K in ((3, 144, 272), (300, 272, 272), (2000, 2048, 272)):       # small and large tiles
+        aq, ascl, wq, wscl, bias = _operands(M, N, K, 21)
+        low, inf = bias.copy(), bias.copy()
+        low[[5, 100]], inf[[5, 100]] = -1e30, (np.inf, np.nan)              # GELU of -1e30 is -0
+        say("gemm_fp8 inf", M, N, K)
+        q0, s0 = _gemm(torch, f3c, 3, aq, ascl, wq, wscl, low)
+        q1, s1 = _gemm(torch, f3c, 3, aq, ascl, wq, wscl, inf)
+        assert np.array_equal(s0, s1) and np.all((q1[:, [5, 100]] & 0x7F) == 0x7F)
+        assert np.array_equal(np.delete(q0, [5, 100], 1), np.delete(q1, [5, 100], 1))
+        assert np.all((q0[:, [5, 100]] & 0x7F) == 0)
+
+
+def test_no_rows(torch, f3c):
+    e = lambda *s, t=torch.uint8: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+    f3c.op_quant_fp8(f3c.F3C_BF16, e(0, 256, t=torch.bfloat16), e(0, 256), e(0, 4))
+    f3c.op_gemm_fp8(0, e(0, 256), e(0, 4), e(128, 256), e(1, 4), out=e(0, 128, t=torch.bfloat16))
+    f3c.op_resid_norm(f3c.F3C_F32, f3c.F3C_F32, e(0, 64, t=torch.float32), out=e(0, 64, t=torch.float32))
+    h = torch.ones(5, 64, device="cuda")
+    f3c.op_resid_norm(f3c.F3C_F32, f3c.F3C_F32, h, y=h.clone(), off=[2, 2, 2], out=e(5, 64, t=torch.float32))
+    torch.cuda.synchronize()
+    assert bool((h == 1).all())
+
+
+def test_rows_far_apart_and_offsets_beyond_32_bits(torch, f3c):
+    """Row strides up to the limit, and rows that start beyond 4 GiB, give the bits of packed rows."""
+    rng = np.random.default_rng(31)
+    M, N, K = 260, 48, 144
+    aq, ascl, wq, wscl, bias = _operands(M, N, K, 30)
+    want = _gemm(torch, f3c, 0, aq, ascl, wq, wscl, bias)
+    ld = (1 << 22) - 16
+    A, W = (torch.empty(n, ld, dtype=torch.uint8, device="cuda")[:, :K] for n in (M, N))
+    A.copy_(to_dev(aq))
+    W.copy_(to_dev(wq))
+    out = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    sa, sw = _scale_dev(torch, f3c, ascl, K), _scale_dev(torch, f3c, wscl, K)
+    say("gemm_fp8 strides", ld)
+    f3c.op_gemm_fp8(0, A, sa, W, sw, to_dev(bias), out=out)
+    assert np.array_equal(out.float().cpu().numpy(), want)
+    # 5 GiB of rows; the last ones hold the values
+    R, ld = 1_100_000, 5120
+    A = torch.zeros(R, ld, dtype=torch.uint8, device="cuda")[:, :K]
+    sa = torch.full((R, 4), 127, dtype=torch.uint8, device="cuda")
+    A[R - M:], sa[R - M:] = to_dev(aq), _scale_dev(torch, f3c, ascl, K)
+    W = to_dev(wq)
+    out = torch.zeros(R, N, dtype=torch.bfloat16, device="cuda")
+    h = torch.zeros(R, 1040, device="cuda")[:, :N]                           # 4.6 GB of residual rows
+    say("gemm_fp8 far", R, ld)
+    f3c.op_gemm_fp8(0, A, sa, W, sw, to_dev(bias), out=out)
+    f3c.op_gemm_fp8(2, A, sa, W, sw, to_dev(bias), resid=h)
+    assert np.array_equal(out[R - M:].float().cpu().numpy(), want)
+    assert torch.equal(h[R - M:].to(torch.bfloat16), out[R - M:])
+    del A, out, h
+    x = torch.zeros(R, 1040, device="cuda")
+    x[R - 3:] = to_dev(rng.standard_normal((3, 1040)).astype(np.float32))
+    q, s = torch.empty(R, 1040, dtype=torch.uint8, device="cuda"), torch.empty(R, 12, dtype=torch.uint8, device="cuda")
+    say("quant far", R)
+    f3c.op_quant_fp8(f3c.F3C_F32, x, q, s)
+    wq_, ws_ = fp8.quantise(x[R - 3:].cpu().numpy())
+    assert np.array_equal(q[R - 3:].cpu().numpy(), wq_) and np.array_equal(s[R - 3:, :9].cpu().numpy(), ws_)
+    o = torch.empty(R, 1040, device="cuda")
+    few = torch.empty(3, 1040, device="cuda")
+    say("resid_norm far", R)
+    f3c.op_resid_norm(f3c.F3C_F32, f3c.F3C_F32, x, y=x, out=o, post=f3c.F3C_NORM_RMS)
+    last = x[R - 3:].clone()
+    f3c.op_resid_norm(f3c.F3C_F32, f3c.F3C_F32, last, out=few)
+    assert torch.equal(o[R - 3:], few)
+    # weights, the second row block beyond 4 GiB
+    w = torch.zeros(130, 8_400_000, device="cuda")[:, :264]
+    w.copy_(to_dev(rng.standard_normal((130, 264)).astype(np.float32)))
+    q, s = torch.empty(130, 264, dtype=torch.uint8, device="cuda"), torch.empty(2, 4, dtype=torch.uint8, device="cuda")
+    f3c.op_quant_fp8(f3c.F3C_F32, w, q, s, block_rows=128)
+    wq_, ws_ = fp8.quantise(w.cpu().numpy(), 128)
+    assert np.array_equal(q.cpu().numpy(), wq_) and np.array_equal(s[:, :3].cpu().numpy(), ws_)
+
+
+def test_calls_on_a_named_stream_and_float8_types(torch, f3c):
+    a = Sublayer(torch, f3c, 70, 256, 9)
+    a.run()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    f8, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    out, so = torch.zeros(70, 1024, dtype=f8, device="cuda"), torch.zeros(70, 8, dtype=e8, device="cuda")
+    torch.cuda.synchronize()
+    f3c.op_gemm_fp8(3, a.u.view(f8), a.us.view(e8), a.q1.view(f8), a.s1.view(e8), a.b1, out=out, out_scale=so,
+                    stream=s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(out.view(torch.uint8), a.hid) and torch.equal(so.view(torch.uint8), a.hs)
+
+
+def _tile(name, M, N, K, epi):
+    """Index of the tile that the library takes (choose_tiles in k_gemm8.hip, with the table as it stands there)."""
+    import math
+    import os
+    import re
+    from paper_2511_22533_amd import build
+    with open(os.path.join(build.CSRC, "k_gemm8.hip")) as f:
+        body = f.read()
+    body = body[body.index(name + "[] = {"):]
+    best = None
+    for i, row in enumerate(re.findall(r"\{([-\d., ]+)\}", body[:body.index("};")])):
+        bm, bn, per_cu, fixed, k, k_round, k_group, k_load, rnd, group, *load_epi = (float(x) for x in row.split(","))
+        if epi == 3 and bn < 128:
+            continue
+        load = math.ceil(M / bm) * math.ceil(N / bn) / 256.0
+        rounds, groups, kt = math.ceil(load / per_cu), math.ceil(load), math.ceil(K / 128)
+        t = fixed + kt * (k + k_round * rounds + k_group * groups + k_load * load) + rnd * rounds + group * groups
+        t += load_epi[(0, 1, 2, 3)[epi]] * load
+        if best is None or t < best[0]:
+            best = (t, i)
+    return best[1]
+
+
+@pytest.mark.parametrize("table,epi,shapes,tiles", [
+    ("kTile8Cost", 0, [(4096, 1024), (1024, 1024), (3600, 144)], 7),
+    ("kTile8Cost", 1, [(4096, 1024), (1024, 1024), (3600, 144)], 7),
+    ("kTile8Cost", 2, [(4096, 1024), (1024, 1024)], 7), ("kTile8Cost", 3, [(4096, 1024), (1024, 1024)], 5),
+    ("kTile8WideCost", 2, [(2048, 4112), (512, 4112)], 5)])
+def test_gemm_tiles_agree_bit_for_bit(torch, f3c, table, epi, shapes, tiles):
+    """Row counts that take each of the tiles (asserted) agree on the rows they share, the largest run's."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    top, crossed = 16000, set()
+    for N, K in shapes:
+        bytes_ = lambda r, c: torch.randint(0, 256, (r, c), generator=g, device="cuda", dtype=torch.uint8)  # noqa: E731
+        code = lambda r, c: (lambda b: torch.where((b & 0x7F) == 0x7F, b - 1, b))(bytes_(r, c))  # noqa: E731
+        A, W = code(top, K), code(N, K)
+        sa = 120 + bytes_(top, f3c.fp8_scale_stride(K)) % 12
+        sw = 110 + bytes_(-(-N // 128), f3c.fp8_scale_stride(K)) % 12
+        bias = torch.randn(N, generator=g, device="cuda")
+
+        def run(m):
+            say("gemm_fp8 tiles", table, epi, m, N, K, _tile(table, m, N, K, epi))
+            so = torch.zeros(m, f3c.fp8_scale_stride(N), dtype=torch.uint8, device="cuda")
+            if epi == 2:
+                o = torch.ones(m, N, device="cuda")
+                f3c.op_gemm_fp8(2, A[:m], sa[:m], W, sw, bias, resid=o)
+            else:
+                o = torch.zeros(m, N, dtype=torch.uint8 if epi == 3 else torch.bfloat16, device="cuda")
+                f3c.op_gemm_fp8(epi, A[:m], sa[:m], W, sw, bias, out=o, out_scale=so if epi == 3 else None)
+            return o, so
+
+        whole = run(top)
+        seen = {_tile(table, top, N, K, epi)}
+        for m in (1, 40, 70, 100, 130, 200, 260, 400, 520, 700, 900, 1300, 1700, 2500, 3300, 4000, 4500, 6000, 8000, 12000):
+            t = _tile(table, m, N, K, epi)
+            if t in seen:
+                continue
+            seen.add(t)
+            for x, y in zip(run(m), whole):
+                assert torch.equal(x, y[:m]), (m, N, K, t)
+        crossed |= seen
+    assert len(crossed) >= tiles, crossed
