@@ -624,21 +624,24 @@ hipError_t launch_dma(const Gemm8Args& a0, hipStream_t s) {
 // round costs a whole one), one per workgroup of the fullest CU and one per 256
 // workgroups' load; per round, workgroup and load the epilogue. A least-squares fit
 // to 1374 measured calls on MI355X (128 to 8192 columns, K = 128 to 8192, 1 to 32768
-// rows, every epilogue): over them its pick is 0.6% slower than the best of the
-// seven in the mean, 23% at worst; they are 0.2% from the best of twelve that were
-// measured. Without the cost per workgroup of a CU it was 1.1% and 41%.
+// rows, every epilogue), each tile where it is within 2.5 times of the best, larger
+// calls weighing a little more: the pick is 0.5% slower than the best of eleven
+// measured tiles in the mean, 25% at worst; for calls over 17 GFLOP 1.1% (with neither
+// 192 x 256 nor 128 x 256 it was 5%: 9831 x 1024 x 4096 56.6 -> 49.7 us).
 struct Tile8Cost {
   int bm, bn, per_cu;
   double fixed, k, k_round, k_group, k_load, round, group, load_store, load_gelu, load_resid, load_fp8;
 };
 constexpr Tile8Cost kTile8Cost[] = {
-    {256, 256, 1, 1.607, 0.548, 0.512, 0.000, 0.816, 4.257, 0.000, 1.899, 6.918, 19.273, 6.561},
-    {128, 128, 4, 2.769, 0.593, 0.000, 0.000, 0.426, 0.000, 1.146, 0.113, 0.756, 3.671, 0.456},
-    {64, 128, 2, 2.329, 0.142, 0.000, 0.153, 0.174, 0.694, 0.491, 0.176, 0.584, 1.963, 0.347},
-    {32, 128, 2, 2.438, 0.033, 0.073, 0.120, 0.125, 0.372, 0.281, 0.000, 0.349, 0.754, 0.191},
-    {64, 64, 2, 2.017, 0.060, 0.076, 0.086, 0.095, 0.524, 0.532, 0.000, 0.202, 0.820, 0.000},
-    {32, 64, 2, 1.653, 0.000, 0.132, 0.057, 0.061, 1.341, 0.053, 0.000, 0.309, 0.558, 0.000},
-    {128, 128, 1, 1.572, 0.119, 0.213, 0.000, 0.348, 2.358, 0.000, 0.000, 1.029, 3.534, 1.167},
+    {256, 256, 1, 4.104, 0.078, 1.252, 0.000, 0.234, 0.500, 0.000, 5.760, 10.001, 22.848, 9.214},
+    {192, 256, 1, 2.124, 0.185, 0.764, 0.000, 0.576, 2.823, 0.000, 1.843, 5.055, 13.074, 4.281},
+    {128, 256, 1, 1.546, 0.073, 0.476, 0.000, 0.503, 3.348, 0.000, 0.489, 2.426, 6.972, 1.916},
+    {128, 128, 4, 2.757, 0.594, 0.000, 0.000, 0.441, 0.000, 1.225, 0.000, 0.588, 3.526, 0.247},
+    {64, 128, 2, 2.288, 0.127, 0.000, 0.170, 0.187, 0.631, 0.624, 0.000, 0.381, 1.609, 0.155},
+    {32, 128, 2, 2.065, 0.089, 0.000, 0.140, 0.145, 0.933, 0.070, 0.000, 0.308, 0.600, 0.123},
+    {64, 64, 2, 1.961, 0.087, 0.027, 0.110, 0.105, 0.727, 0.385, 0.000, 0.201, 0.704, 0.000},
+    {32, 64, 2, 1.812, 0.000, 0.136, 0.053, 0.069, 1.162, 0.086, 0.000, 0.301, 0.380, 0.000},
+    {128, 128, 1, 1.730, 0.094, 0.237, 0.000, 0.377, 2.182, 0.000, 0.000, 0.971, 3.287, 1.046},
 };
 
 // The same for products on bf16 instructions, residual epilogue: a fit to 272 calls
@@ -696,16 +699,18 @@ hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   }
   switch (choose_tiles(kTile8Cost, a.M, a.N, a.K, EPI)) {
     case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1>(a, s);
-    case 1: return launch_dma<128, 128, 2, 2, 1, 4, EPI, 4>(a, s);
-    case 2: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2>(a, s);
-    case 3: return launch_dma<32, 128, 1, 4, 3, 2, EPI, 4>(a, s);
-    case 4:
+    case 1: return launch_dma<192, 256, 2, 4, 2, 2, EPI, 1>(a, s);
+    case 2: return launch_dma<128, 256, 2, 4, 3, 2, EPI, 1>(a, s);
+    case 3: return launch_dma<128, 128, 2, 2, 1, 4, EPI, 4>(a, s);
+    case 4: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2>(a, s);
+    case 5: return launch_dma<32, 128, 1, 4, 3, 2, EPI, 4>(a, s);
+    case 6:
       if constexpr (EPI != EPI_GELU_FP8) return launch_dma<64, 64, 2, 2, 4, 2, EPI, 4>(a, s);
       break;
-    case 5:
+    case 7:
       if constexpr (EPI != EPI_GELU_FP8) return launch_dma<32, 64, 1, 2, 5, 1, EPI, 4>(a, s);
       break;
-    case 6: return launch_dma<128, 128, 2, 4, 4, 2, EPI, 1>(a, s);
+    case 8: return launch_dma<128, 128, 2, 4, 4, 2, EPI, 1>(a, s);
   }
   return hipErrorInvalidValue;
 }
