@@ -561,24 +561,28 @@ def _device(t, torch) -> int:
 def _rows(name: str, t, types, rows: int, cols: int, dev: int):
     """(address, row stride) of t, rows x cols of one of these types with contiguous columns. A single row's stride
     says nothing: then its length, rounded up to 16 bytes."""
-    if t.dtype not in types or t.get_device() != dev or t.shape != (rows, cols):
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {types[0]} {(rows, cols)} on "
-                         f"the current GPU")
-    ld, step = t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError(f"{name}: rows with contiguous columns expected")
-    if rows < 2:
-        unit = 16 // t.element_size()
-        ld = (cols + unit - 1) // unit * unit
-    return t.data_ptr(), ld
+    if t.dtype in types and t.shape == (rows, cols) and t.get_device() == dev:
+        ld, step = t.stride()
+        if step == 1 or cols < 2:
+            if rows < 2:
+                unit = 16 // t.element_size()
+                ld = (cols + unit - 1) // unit * unit
+            return t.data_ptr(), ld
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}, expected {types[0]} "
+                     f"{(rows, cols)} with contiguous columns on the current GPU")
 
 
 def _scale_rows(name: str, t, types, rows: int, cols: int, dev: int):
     """The same for the scales of `cols` columns, whose rows may be longer."""
     need = ((cols + 127) // 128 + 3) // 4 * 4
-    if t.dim() != 2 or t.shape[1] < need:
-        raise ValueError(f"{name}: {tuple(t.shape)}, expected [{rows}][{need} or more]")
-    return _rows(name, t, types, rows, t.shape[1], dev)
+    if t.dim() == 2:
+        n, width = t.shape
+        if n == rows and width >= need and t.dtype in types and t.get_device() == dev:
+            ld, step = t.stride()
+            if step == 1:
+                return t.data_ptr(), ld if rows > 1 else need
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}, expected {types[0]} "
+                     f"[{rows}][{need} or more] with contiguous columns on the current GPU")
 
 
 def _vector(name: str, t, types, n: int, dev: int):
