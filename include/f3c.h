@@ -401,8 +401,8 @@ int f3c_op_ln_mod(int32_t dtype, int32_t rows, int32_t d, const float* h, const 
  * block is the smallest 2^e, e in [-126, 127], with |x| <= 448 * 2^e for all its
  * finite x (2^-126 if there is none but zeros); q = x * 2^-e, an exact product,
  * rounded to nearest even. NaN and infinities become NaN and do not count for
- * the scale. K a multiple of 8; x and q rows 16- and 8-byte aligned; fewer than
- * 2^28 blocks of 1 x 128 or 2^24 of 128 x 128. Errors: F3C_EINVAL (dtype,
+ * the scale. K a multiple of 8, below 2^30; x and q rows 16- and 8-byte aligned; at
+ * most 2^28 - 16 blocks of 1 x 128, fewer than 2^24 of 128 x 128. Errors: F3C_EINVAL (dtype,
  * block_rows, shape, leading dims, NULL or misaligned pointers). */
 int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K, const void* x, int32_t ldx, void* q,
                      int32_t ldq, void* scale, int32_t lds, f3c_stream stream);
@@ -418,10 +418,11 @@ int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K,
  * of its size where the operands are normally distributed and by 2e-5 where A
  * holds GELU's outputs; into a float32 residual, sums of K > 4096 are formed from
  * exact products on bf16 instructions instead, at half the rate (1.4e-7). N and K
- * multiples of 16, M and N below 2^30; rows of A, W, out and resid 16-byte
- * aligned, of bias and gate too; lda, ldw, ldsa, ldsw below 2^22. The result of an
- * output row does not depend on M or on other rows, nor on scheduling. out,
- * out_scale and resid must not overlap the operands. Errors: F3C_EINVAL. */
+ * multiples of 16, M and N below 2^30, ceil(M/32) * ceil(N/64) below 2^24 - 1;
+ * rows of A, W, out and resid 16-byte aligned, of bias and gate too; lda, ldw,
+ * ldsa, ldsw below 2^22. The result of an output row does not depend on M or on
+ * other rows, nor on scheduling. out, out_scale and resid must not overlap the
+ * operands. Errors: F3C_EINVAL. */
 int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,
                     const void* A_scale, int32_t ldsa, const void* W, int32_t ldw, const void* W_scale, int32_t ldsw,
                     const float* bias, const float* gate, void* out, int32_t ldo, void* out_scale, int32_t ldso,

@@ -983,7 +983,7 @@ int f3c_op_gemm(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K
   if ((K * es) % 128) return fail(F3C_EINVAL, "K must be a multiple of %d", 128 / es);
   if (lda < K || ldw < K || (lda * es) % 16 || (ldw * es) % 16) return fail(F3C_EINVAL, "bad leading dims");
   if (!A || !W || !bias) return fail(F3C_EINVAL, "NULL operand");
-  if (epilogue == 2 ? ((M && !resid) || ldr < N || ldr % 4) : (!out || ldo < N || ldo % 4))
+  if (epilogue == 2 ? (!resid || ldr < N || ldr % 4) : (!out || ldo < N || ldo % 4))
     return fail(F3C_EINVAL, "bad output (leading dim below N or not a multiple of 4)");
   HIP_TRY(launch_gemm(SITE_OP, dtype, epilogue, M, N, K, A, lda, W, ldw, bias, gate, out, ldo, resid, ldr,
                       (hipStream_t)stream));
@@ -1082,13 +1082,15 @@ int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K,
                      int32_t ldq, void* scale, int32_t lds, f3c_stream stream) {
   if (dtype != F3C_F32 && dtype != F3C_BF16) return fail(F3C_EINVAL, "bad dtype");
   if (block_rows != 1 && block_rows != 128) return fail(F3C_EINVAL, "block_rows must be 1 or 128");
-  if (rows < 0 || K <= 0 || K % 8) return fail(F3C_EINVAL, "bad shape (K must be a multiple of 8)");
+  if (rows < 0 || K <= 0 || K % 8 || K >= (1 << 30))
+    return fail(F3C_EINVAL, "bad shape (K must be a multiple of 8, below 2^30)");
   if (rows && (!x || !q)) return fail(F3C_EINVAL, "NULL argument");
   if (ldx < K || ldq < K || !aligned_rows(x, ldx, dtype == F3C_BF16 ? 2 : 4, 16) || !aligned_rows(q, ldq, 1, 8))
     return fail(F3C_EINVAL, "bad leading dims or alignment (x rows 16 bytes, q rows 8)");
   if (int rc = check_scales("scale", scale, lds, K, rows)) return rc;
   const int64_t blocks = ((int64_t)rows + block_rows - 1) / block_rows * (((int64_t)K + 127) / 128);
-  if (blocks >= (block_rows == 1 ? 1 << 28 : 1 << 24)) return fail(F3C_EINVAL, "too many blocks for one launch");
+  // (a launch has fewer than 2^32 threads, in whole workgroups)
+  if (blocks > (block_rows == 1 ? (1 << 28) - 16 : (1 << 24) - 1)) return fail(F3C_EINVAL, "too many blocks for one launch");
   HIP_TRY(launch_quant_fp8(dtype, block_rows, rows, K, x, ldx, q, ldq, scale, lds, (hipStream_t)stream));
   return F3C_OK;
 }
@@ -1099,6 +1101,9 @@ int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const voi
                     float* resid, int32_t ldr, f3c_stream stream) {
   if (epilogue < EPI_STORE || epilogue > EPI_GELU_FP8) return fail(F3C_EINVAL, "bad epilogue");
   if (M < 0 || N <= 0 || K <= 0 || M >= (1 << 30) || N >= (1 << 30)) return fail(F3C_EINVAL, "bad shape");
+  // (a launch has fewer than 2^32 threads: 256 for the smallest tiles at most)
+  if ((int64_t)((M + 31) / 32) * ((N + 63) / 64) >= (1 << 24) - 1)
+    return fail(F3C_EINVAL, "too many outputs for one launch");
   if (N % 16 || K % 16) return fail(F3C_EINVAL, "N and K must be multiples of 16");
   if ((M && !A) || !W) return fail(F3C_EINVAL, "NULL operand");
   if (lda < K || ldw < K || !aligned_rows(A, lda, 1, 16) || !aligned_rows(W, ldw, 1, 16))

@@ -81,6 +81,22 @@ def test_resid_norm_refuses(cfg, kw):
     assert _norm(null_cfg=True) == f3c.F3C_EINVAL
 
 
+@pytest.mark.parametrize("call,kw", [
+    # 2^32 threads, or a block count past 32 bits
+    (_quant, dict(rows=(1 << 28) - 15, K=128, ldx=128, ldq=128)),
+    (_quant, dict(rows=(1 << 26) - 3, K=512, ldx=512, ldq=512)),
+    (_quant, dict(rows=1, K=(1 << 31) - 8, ldx=(1 << 31) - 8, ldq=(1 << 31) - 8, lds=1 << 24)),
+    (_quant, dict(rows=1, K=1 << 30, ldx=1 << 30, ldq=1 << 30, lds=1 << 23, block_rows=128)),
+    (_quant, dict(rows=(1 << 31) - 1, K=128, ldx=128, ldq=128, lds=4, block_rows=128)),
+    (_gemm, dict(M=(1 << 30) - 1, N=16, K=16)),
+    (_gemm, dict(M=(1 << 29) + 1, N=64, K=16)),
+    (_gemm, dict(M=1, N=(1 << 30) - 16, ldo=(1 << 30) - 16)),
+    (_gemm, dict(M=1 << 25, N=1 << 10, K=128, ldo=1 << 10))])
+def test_more_than_a_launch_holds_is_refused(call, kw):
+    assert call(**kw) == f3c.F3C_EINVAL
+    assert f3c.lib().f3c_last_error()
+
+
 def test_no_rows_is_no_work():
     assert _quant(rows=0, x=None, q=None, scale=None) == f3c.F3C_OK
     assert _gemm(M=0, A=None, sa=None, out=None) == f3c.F3C_OK
