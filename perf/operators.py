@@ -261,8 +261,8 @@ def _run_norm(s):
         codes = {"f32": f3c.F3C_F32, "bf16": f3c.F3C_BF16, "fp8": f3c.F3C_FP8}
         f3c.op_resid_norm(codes[case["dtype"]], codes[case["out"]], s["h"], y=s["y"], off=s["off"], out=s["out"],
                           out_scale=s.get("out_scale"), post=NORMS[case["post"]], pre=NORMS[case["pre"]],
-                          post_w=s.get("post_w"), pre_w=s.get("pre_w"), gate=s["gate"], resid_scale=RESID_SCALE,
-                          shift=s["shift"], scale=s["scale"])
+                          post_w=s.get("post_w") if case["post"] != "none" else None, pre_w=s.get("pre_w"),
+                          gate=s["gate"], resid_scale=RESID_SCALE, shift=s["shift"], scale=s["scale"])
         out = {"h": s["h"], "out": s["out"]}
         return dict(out, scale=_scales(s["out_scale"], case["d"])) if case["out"] == "fp8" else out
     rows = torch.tensor([b - a for a, b in zip(s["off"], s["off"][1:])], device=DEV)
