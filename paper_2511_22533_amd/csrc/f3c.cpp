@@ -18,6 +18,7 @@
 #include "../../include/f3c.h"
 #include "common.h"
 #include "kernels.h"
+#include "kernels8.h"
 
 using namespace f3c;
 

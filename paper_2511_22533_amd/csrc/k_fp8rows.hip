@@ -7,7 +7,7 @@
 // us, 4.7, with as much written as read. Under some 20 MB the 1.9 us of a launch and
 // one round trip to memory count as much: 9831 x 1024 5.7 us, 820 rows of the pass 5.3.
 #include "fp8.h"
-#include "kernels.h"
+#include "kernels8.h"
 
 namespace f3c {
 

@@ -22,7 +22,7 @@
 #include <type_traits>
 
 #include "fp8.h"
-#include "kernels.h"
+#include "kernels8.h"
 
 namespace f3c {
 
@@ -277,7 +277,7 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // chain of K tiles, 0.2 to 0.3 us each, of LDS reads and two dependent products.
 // Against the bf16 projections on one box (us, bf16 / here): 32768 x 4096 x 1024 GELU
 // 283 / 154 (out in 8 bits), 32768 x 1024 x 4096 residual 264 / 147, 9831 x 2048 x 1024
-// 52 / 28, 9831 x 1024 x 4096 residual 88 / 57, 820 x 1024 x 4096 residual 19 / 12.6.
+// 52 / 28, 9831 x 1024 x 4096 residual 88 / 50, 820 x 1024 x 4096 residual 19 / 12.6.
 template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, bool WIDE = false>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;

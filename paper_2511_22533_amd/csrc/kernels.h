@@ -17,9 +17,8 @@ struct Segs {
   int off[kMaxBatch + 1];
 };
 
-enum Dtype { DT_F32 = 0, DT_BF16 = 1, DT_FP8 = 2 };
-enum Epilogue { EPI_STORE = 0, EPI_GELU = 1, EPI_RESID = 2, EPI_GELU_FP8 = 3 };
-enum Norm { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };
+enum Dtype { DT_F32 = 0, DT_BF16 = 1 };
+enum Epilogue { EPI_STORE = 0, EPI_GELU = 1, EPI_RESID = 2 };
 
 // Call sites of the dense kernels. Each site is its own template instance, so a
 // kernel trace attributes time to the projection / attention it belongs to.
@@ -104,29 +103,6 @@ hipError_t launch_convert(int dt, const float* src, void* dst, int64_t n, hipStr
 hipError_t launch_gemm(int site, int dt, int epi, int M, int N, int K, const void* A, int lda, const void* W,
                        int ldw, const float* bias, const float* gate, void* out, int ldo, float* resid, int ldr,
                        hipStream_t s, float oscale = 1.0f, int oscale_cols = 0);
-
-// The same on e4m3 operands with E8M0 scales: sa [M][ldsa] per 1 x 128 of A, sw
-// [ceil(N/128)][ldsw] per 128 x 128 of W (row strides multiples of 4); bias may
-// be null. EPI_GELU_FP8 writes out as e4m3 and so [M][ldso]. N, K and row strides
-// of 8-bit operands multiples of 16.
-hipError_t launch_gemm_fp8(int epi, int M, int N, int K, const void* A, int64_t lda, const void* sa, int64_t ldsa,
-                           const void* W, int64_t ldw, const void* sw, int64_t ldsw, const float* bias,
-                           const float* gate, void* out, int64_t ldo, void* so, int64_t ldso, float* resid,
-                           int64_t ldr, hipStream_t s);
-
-// e4m3 values and E8M0 scales of x [rows][K] (f32 or bf16) per block_rows (1 or
-// 128) x 128; K a multiple of 8.
-hipError_t launch_quant_fp8(int dt, int block_rows, int rows, int K, const void* x, int64_t ldx, void* q, int64_t ldq,
-                            void* scale, int64_t lds, hipStream_t s);
-
-// h += rs * gate * (post(y) * post_w) (y null: h as it is), out = (pre(h) *
-// pre_w) * (1 + scale) + shift (out null: none) over the rows of the segments;
-// gate, shift, scale [B][ldm]; null factors are left out. d a multiple of 8, at
-// most 8192.
-hipError_t launch_resid_norm(int dt, int out_dt, int post, int pre, float eps, float resid_scale, int d,
-                             const Segs& rows, const void* y, int64_t ldy, const float* post_w, const float* gate,
-                             float* h, int64_t ldh, const float* pre_w, const float* shift, const float* scale,
-                             int64_t ldm, void* out, int64_t ldo, void* out_scale, int64_t lds, hipStream_t s);
 
 // Varlen multi-head softmax attention. Queries of sample b are rows
 // [qs.off[b], qs.off[b+1]) of q; its keys/values are rows [ks.off[b], ks.off[b+1])
