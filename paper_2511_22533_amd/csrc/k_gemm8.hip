@@ -276,8 +276,8 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // of 128 x 128 in a single stage 157. Into a residual it is its 268 MB. Few rows: the
 // chain of K tiles, 0.2 to 0.3 us each, of LDS reads and two dependent products.
 // Against the bf16 projections on one box (us, bf16 / here): 32768 x 4096 x 1024 GELU
-// 283 / 154 (out in 8 bits), 32768 x 1024 x 4096 residual 264 / 147, 9831 x 2048 x 1024
-// 52 / 28, 9831 x 1024 x 4096 residual 88 / 50, 820 x 1024 x 4096 residual 19 / 12.6.
+// 297 / 155 (out in 8 bits), 32768 x 1024 x 4096 residual 267 / 149, 9831 x 2048 x 1024
+// 55 / 29, 9831 x 1024 x 4096 residual 93 / 50, 820 x 1024 x 4096 residual 19 / 12.
 template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, bool WIDE = false>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
