@@ -276,8 +276,8 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // of 128 x 128 in a single stage 157. Into a residual it is its 268 MB. Few rows: the
 // chain of K tiles, 0.2 to 0.3 us each, of LDS reads and two dependent products.
 // Against the bf16 projections on one box (us, bf16 / here): 32768 x 4096 x 1024 GELU
-// 297 / 155 (out in 8 bits), 32768 x 1024 x 4096 residual 267 / 149, 9831 x 2048 x 1024
-// 55 / 29, 9831 x 1024 x 4096 residual 93 / 50, 820 x 1024 x 4096 residual 19 / 12.
+// 297 / 157 (out in 8 bits), 32768 x 1024 x 4096 gated residual 266 / 151, 9831 x 2048
+// x 1024 55 / 29, 9831 x 1024 x 4096 gated residual 93 / 50, of 820 rows 19 / 12.
 template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, bool WIDE = false>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
@@ -677,16 +677,18 @@ inline int choose_tiles(const Tile8Cost (&cost)[COUNT], int M, int N, int K, int
 
 // The residual is float32, and v's own error (2e-5 of it behind a GELU) reaches the
 // residual's in proportion to v, which grows with sqrt(K): for rows of size 1 and
-// weights of size 0.02, 0.9e-5 at K = 4096, 1.2e-5 at 8192. Beyond 4096 the residual
-// epilogue therefore multiplies on bf16 instructions, exact products at half the
-// rate: 8e-8. 16384 x 1024 x 8192 146 -> 217 us, 820 x 2048 x 8192 29 -> 44. (The
-// other epilogues round to bf16 or e4m3 behind it, 200 times as much.)
-constexpr int kResidWideK = 4096;
+// weights of size 0.02, 6.8e-6 at K = 2048 and 9.1e-6 at 4096 (up to 1.2e-5 in single
+// rows), behind a gate of size 0.5 half of that, 1.2e-5 at 8192. To stay below 1e-5 the
+// residual epilogue multiplies beyond 4096, without a gate beyond 2048, on bf16
+// instructions, exact products at half the rate: 8e-8. 16384 x 1024 x 8192 146 -> 217 us,
+// 820 x 2048 x 8192 29 -> 44, 32768 x 1024 x 4096 without a gate 151 -> 230. (The other
+// epilogues round to bf16 or e4m3 behind it, 200 times as much.)
+constexpr int kResidWideK = 4096, kResidWideKNoGate = 2048;
 
 template <int EPI>
 hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   if constexpr (EPI == EPI_RESID) {
-    if (a.K > kResidWideK) {
+    if (a.K > (a.gate ? kResidWideK : kResidWideKNoGate)) {
       switch (choose_tiles(kTile8WideCost, a.M, a.N, a.K, EPI)) {
         case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1, true>(a, s);
         case 1: return launch_dma<128, 128, 2, 2, 1, 2, EPI, 4, true>(a, s);

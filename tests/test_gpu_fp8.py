@@ -229,10 +229,12 @@ def test_gemm_scales_far_apart(torch, f3c, epi):
     _check_gemm(torch, f3c, epi, _operands(40, 144, 1280, 6, spread=18.0))
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 128, 4112), (40, 144, 4240), (200, 272, 4112), (700, 528, 4112)])
+@pytest.mark.parametrize("M,N,K", [(1, 128, 4112), (40, 144, 4240), (200, 272, 4112), (700, 528, 4112),
+                                   (1, 128, 2064), (64, 1024, 4096), (300, 512, 2432), (2000, 1024, 4096)])
 def test_gemm_residual_of_long_sums_is_exact(torch, f3c, M, N, K):
-    """Beyond K = 4096 the residual epilogue's products are exact and its sums float32: each of the K / 16 additions to
-    the accumulator (and those within an instruction, 16 at a time) is off by 2^-23 at most of the sum of magnitudes."""
+    """Beyond K = 2048 (4096 with a gate) the residual epilogue's products are exact and its sums float32: each of the
+    K / 16 additions to the accumulator (and those within an instruction, 16 at a time) is off by 2^-23 at most of the
+    sum of magnitudes."""
     say("gemm_fp8 wide", M, N, K)
     aq, ascl, wq, wscl, bias = _operands(M, N, K, 12)
     ascl[M // 2, 3], ascl[0, 1] = 255, 0                 # a NaN scale, and the smallest
