@@ -10,6 +10,7 @@ If the library has not been built, ``lib()`` raises: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 from typing import Dict, Optional, Sequence
@@ -588,9 +589,20 @@ def _scale_rows(name: str, t, types, rows: int, cols: int, dev: int):
 def _vector(name: str, t, types, n: int, dev: int):
     if t is None:
         return None
-    if t.dtype not in types or t.get_device() != dev or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+    if t.dtype not in types or t.get_device() != dev or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name}: {n} contiguous float32 values on the current GPU expected")
     return t.data_ptr()
+
+
+def _per_sample(name: str, t, types, B: int, n: int, dev: int):
+    """(address, row stride) of t [B][n], or [n] for all samples: stride 0. Strides of None and of one sample say
+    nothing: None and 0."""
+    if t is None:
+        return None, None
+    if t.dim() == 1:
+        return _vector(name, t, types, n, dev), 0
+    ptr, ld = _rows(name, t, types, B, n, dev)
+    return ptr, 0 if B == 1 else ld
 
 
 def _stream_on(stream, dev: int, torch) -> int:
@@ -640,6 +652,18 @@ def op_gemm_fp8(epilogue: int, A, A_scale, W, W_scale, bias=None, out=None, out_
         *(none if resid is None else _rows("resid", resid, f32, M, N, dev)), _stream_on(stream, dev, T["torch"])))
 
 
+@functools.lru_cache(maxsize=256)
+def _resid_norm_cfg(*fields):
+    """The C structure of these values, which no call changes."""
+    return ctypes.byref(ResidNormCfg(*fields))
+
+
+@functools.lru_cache(maxsize=256)
+def _offsets(off: tuple):
+    """Row offsets as the C array that no call changes, the number of samples, the lowest and the highest offset."""
+    return _i32(off), len(off) - 1, min(off, default=0), max(off, default=0)
+
+
 def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out_scale=None, post: int = F3C_NORM_NONE,
                   pre: int = F3C_NORM_LAYER, post_w=None, pre_w=None, gate=None, resid_scale: float = 1.0, shift=None,
                   scale=None, eps: float = 1e-6, stream=None):
@@ -650,33 +674,23 @@ def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out
     if dtype not in (F3C_F32, F3C_BF16) or out_dtype not in (F3C_F32, F3C_BF16, F3C_FP8) or h.dim() != 2:
         raise ValueError("rows h, dtype F3C_F32 or F3C_BF16, out_dtype F3C_F32, F3C_BF16 or F3C_FP8 expected")
     R, d = h.shape
-    off = (0, R) if off is None else off
-    B = len(off) - 1
-    if B < 1 or min(off) < 0 or max(off) > R:
+    offsets, B, lowest, highest = _offsets((0, R) if off is None else tuple(map(int, off)))
+    if B < 1 or lowest < 0 or highest > R:
         raise ValueError("off: B + 1 row offsets within h expected")
     if (out_scale is None) == (out is not None and out_dtype == F3C_FP8):
         raise ValueError("out_scale goes with F3C_FP8 rows")
     dev = _device(h, T["torch"])
     none, f32 = (None, 0), T[F3C_F32]
-    mods, ldm = [], None
-    for name, t in (("gate", gate), ("shift", shift), ("scale", scale)):
-        if t is None:
-            mods.append(None)
-            continue
-        if t.dim() == 1:
-            ptr, ld = _vector(name, t, f32, d, dev), 0
-        else:
-            ptr, ld = _rows(name, t, f32, B, d, dev)
-            ld = 0 if B == 1 else ld
-        if ldm is not None and ld != ldm:
-            raise ValueError("gate, shift and scale must have one row stride")
-        mods.append(ptr)
-        ldm = ld
-    c = ResidNormCfg(dtype, out_dtype, post, pre, eps, resid_scale)
+    gate, ldg = _per_sample("gate", gate, f32, B, d, dev)
+    shift, ldm = _per_sample("shift", shift, f32, B, d, dev)
+    scale, lds = _per_sample("scale", scale, f32, B, d, dev)
+    if ldm != lds or (ldg is not None and ldm is not None and ldg != ldm):
+        raise ValueError("gate, shift and scale must have one row stride, and shift and scale go together")
     check((_lib or lib()).f3c_op_resid_norm(
-        ctypes.byref(c), d, B, (c_int * (B + 1))(*off), *(none if y is None else _rows("y", y, T[dtype], R, d, dev)),
-        _vector("post_w", post_w, f32, d, dev), mods[0], *_rows("h", h, f32, R, d, dev),
-        _vector("pre_w", pre_w, f32, d, dev), mods[1], mods[2], ldm or 0,
+        _resid_norm_cfg(dtype, out_dtype, post, pre, eps, resid_scale), d, B, offsets,
+        *(none if y is None else _rows("y", y, T[dtype], R, d, dev)), _vector("post_w", post_w, f32, d, dev), gate,
+        *_rows("h", h, f32, R, d, dev), _vector("pre_w", pre_w, f32, d, dev), shift, scale,
+        (ldg if ldm is None else ldm) or 0,
         *(none if out is None else _rows("out", out, T[out_dtype], R, d, dev)),
         *(none if out_scale is None else _scale_rows("out_scale", out_scale, T["scale"], R, d, dev)),
         _stream_on(stream, dev, T["torch"])))
