@@ -653,12 +653,6 @@ def op_gemm_fp8(epilogue: int, A, A_scale, W, W_scale, bias=None, out=None, out_
 
 
 @functools.lru_cache(maxsize=256)
-def _resid_norm_cfg(*fields):
-    """The C structure of these values, which no call changes."""
-    return ctypes.byref(ResidNormCfg(*fields))
-
-
-@functools.lru_cache(maxsize=256)
 def _offsets(off: tuple):
     """Row offsets as the C array that no call changes, the number of samples, the lowest and the highest offset."""
     return _i32(off), len(off) - 1, min(off, default=0), max(off, default=0)
@@ -687,7 +681,7 @@ def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out
     if ldm != lds or (ldg is not None and ldm is not None and ldg != ldm):
         raise ValueError("gate, shift and scale must have one row stride, and shift and scale go together")
     check((_lib or lib()).f3c_op_resid_norm(
-        _resid_norm_cfg(dtype, out_dtype, post, pre, eps, resid_scale), d, B, offsets,
+        ctypes.byref(ResidNormCfg(dtype, out_dtype, post, pre, eps, resid_scale)), d, B, offsets,
         *(none if y is None else _rows("y", y, T[dtype], R, d, dev)), _vector("post_w", post_w, f32, d, dev), gate,
         *_rows("h", h, f32, R, d, dev), _vector("pre_w", pre_w, f32, d, dev), shift, scale,
         (ldg if ldm is None else ldm) or 0,

@@ -126,3 +126,31 @@ def test_bindings_refuse_what_does_not_fit():
 
 def test_scale_stride():
     assert [f3c.fp8_scale_stride(n) for n in (1, 128, 129, 512, 513, 1024)] == [4, 4, 4, 4, 8, 8]
+
+
+def test_resid_norm_takes_scalars_as_they_are_at_the_call(monkeypatch):
+    """Scalars held in a tensor or an array that changes between calls, and zeros of either sign, reach the library with
+    the values that they have at each call."""
+    import torch
+    got = []
+
+    class Library:
+        def f3c_op_resid_norm(self, cfg, *rest):
+            got.append((cfg._obj.eps, cfg._obj.resid_scale))
+            return f3c.F3C_OK
+
+    monkeypatch.setattr(f3c, "_lib", Library())
+    monkeypatch.setattr(f3c, "_device", lambda t, torch: t.get_device())
+    monkeypatch.setattr(f3c, "_stream_on", lambda *a: 0)
+    h = torch.zeros(2, 8)
+    call = lambda **kw: f3c.op_resid_norm(f3c.F3C_F32, f3c.F3C_F32, h, y=h, **kw)  # noqa: E731
+    for scale, eps in ((torch.tensor(0.5), torch.tensor(0.25)), (np.array(0.5), np.array(0.25))):
+        got.clear()
+        call(resid_scale=scale, eps=eps)
+        scale[...], eps[...] = 2.0, 0.125
+        call(resid_scale=scale, eps=eps)
+        assert got == [(0.25, 0.5), (0.125, 2.0)]
+    got.clear()
+    call(resid_scale=0.0)
+    call(resid_scale=-0.0)
+    assert [np.signbit(s) for _, s in got] == [False, True]
