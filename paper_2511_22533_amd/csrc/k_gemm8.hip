@@ -675,20 +675,20 @@ inline int choose_tiles(const Tile8Cost (&cost)[COUNT], int M, int N, int K, int
   return best;
 }
 
-// The residual is float32, and v's own error (2e-5 of it behind a GELU) reaches the
-// residual's in proportion to v, which grows with sqrt(K): for rows of size 1 and
-// weights of size 0.02, 6.8e-6 at K = 2048 and 9.1e-6 at 4096 (up to 1.2e-5 in single
-// rows), behind a gate of size 0.5 half of that, 1.2e-5 at 8192. To stay below 1e-5 the
-// residual epilogue multiplies beyond 4096, without a gate beyond 2048, on bf16
-// instructions, exact products at half the rate: 8e-8. 16384 x 1024 x 8192 146 -> 217 us,
-// 820 x 2048 x 8192 29 -> 44, 32768 x 1024 x 4096 without a gate 151 -> 230. (The other
-// epilogues round to bf16 or e4m3 behind it, 200 times as much.)
-constexpr int kResidWideK = 4096, kResidWideKNoGate = 2048;
+// The residual is float32, and v's own error (1.5e-5 of it, 2.1e-5 behind a GELU) reaches
+// it times the gate, whose size only the device knows. v grows with sqrt(K): for
+// normally distributed rows of size 1, weights of size 0.02 and no gate or one of size 1
+// the residual is 8.0e-6 off at K = 1024 and 1.0e-5 (1.2e-5 in single rows) at 2048;
+// behind a GELU 4.9e-6 and 6.8e-6. Beyond 2048 this epilogue multiplies on bf16
+// instructions, exact products at half the rate: 7e-8 of the residual at K = 4096, 1.1e-7
+// at 8192. (The other epilogues round to bf16 or e4m3 behind the sum, over 100 times as
+// much.)
+constexpr int kResidWideK = 2048;
 
 template <int EPI>
 hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   if constexpr (EPI == EPI_RESID) {
-    if (a.K > (a.gate ? kResidWideK : kResidWideKNoGate)) {
+    if (a.K > kResidWideK) {
       switch (choose_tiles(kTile8WideCost, a.M, a.N, a.K, EPI)) {
         case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1, true>(a, s);
         case 1: return launch_dma<128, 128, 2, 2, 1, 2, EPI, 4, true>(a, s);

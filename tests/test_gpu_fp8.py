@@ -712,3 +712,32 @@ def test_gemm_8_bit_sums_are_as_exact_as_stated(torch, f3c, rows, K):
     got = _residual(torch, f3c, aq, ascl, wq, wscl)
     assert _rel(got, fp8.linear(fp8.dequantise(aq, ascl), fp8.dequantise(wq, wscl, 128))) <= (
         3e-5 if rows == "gelu" else 2e-5)
+
+
+@pytest.mark.parametrize("K", [512, 2048, 2064, 4096, 4112])
+def test_gemm_gate_of_ones_is_no_gate(torch, f3c, K):
+    """The same bits, and with them the same accuracy."""
+    aq, ascl, wq, wscl, _ = _operands(70, 144, K, K)
+    h = np.random.default_rng(2).standard_normal((70, 144)).astype(np.float32)
+    say("gemm_fp8 gate of ones", K)
+    one, none = (_residual(torch, f3c, aq, ascl, wq, wscl, gate=g, h=h) for g in (np.ones(144, np.float32), None))
+    assert np.array_equal(one, none)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", [(1, 128, 2064), (1, 128, 4112), (1, 1024, 4096), (40, 144, 2064), (300, 512, 4096),
+                                   (200, 272, 4112), (1500, 1024, 4096)])
+def test_gemm_residual_of_long_sums_with_gates(torch, f3c, gated, M, N, K):
+    """Beyond K = 2048 products are exact and sums float32, whatever the gate's size: each of K / 16 additions to the
+    accumulator and of those within an instruction is off by 2^-23 of the sum of magnitudes at most, and in the 2-norm,
+    where they do not all fall to one side, by 2^-23 times the root of their number of the sum itself."""
+    aq, ascl, wq, wscl, _ = _operands(M, N, K, M + K, spread=0.0)
+    rng = np.random.default_rng(N)
+    gate = (rng.standard_normal(N) * np.exp2(rng.uniform(-4, 4, N))).astype(np.float32) if gated else None
+    a, w = fp8.dequantise(aq, ascl), fp8.dequantise(wq, wscl, 128)
+    g = 1.0 if gate is None else gate.astype(np.float64)
+    want, tot = g * fp8.linear(a, w), np.abs(g) * (np.abs(a) @ np.abs(w).T)
+    say("gemm_fp8 long sums", M, N, K, gated)
+    got = _residual(torch, f3c, aq, ascl, wq, wscl, gate=gate)
+    assert np.all(np.abs(got - want) <= (K / 16 + 16) * 2.0 ** -23 * tot + 2.0 ** -22 * np.abs(want))
+    assert _rel(got, want) <= np.sqrt(K / 16 + 16) * 2.0 ** -23 + 2.0 ** -23
