@@ -65,10 +65,17 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// 2^(byte - 127) of the lowest byte; 255 is NaN.
-__device__ __forceinline__ float widen_scale(uint32_t s) {
-  s &= 0xffu;
-  return __builtin_bit_cast(float, s == 0 ? 0x00400000u : s == 255 ? 0x7fc00000u : s << 23);
+// A block's two scales (bytes; 255 is NaN) as one for widen8 on the activations, beside
+// 2^27 on the weights. No value leaves bf16's range above: an exponent over 119 is
+// taken for 119, whose products with any weight but 0 (2^-9 at least) leave float32's
+// range all the same. Below, products under 2^-81 may be lost. (Each operand under its
+// own scale, values over 2^128 became infinities and those under 2^-133 zeros,
+// whatever the other operand's scale.)
+constexpr float kWideWeightScale = 0x1p27f;
+__device__ __forceinline__ float wide_row_scale(uint32_t sa, uint32_t sw) {
+  sa &= 0xffu, sw &= 0xffu;
+  const int e = min(max((int)(sa + sw) - 254 - 27, -126), 119);
+  return __builtin_bit_cast(float, sa == 255 || sw == 255 ? 0x7fc00000u : (uint32_t)(e + 127) << 23);
 }
 
 // Epilogue through LDS, 32 rows of the wave at a time (a lane of the MFMA layout
@@ -395,6 +402,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   union Frag { i32x8 v; u32x4 h[2]; };
   Frag fa[TM], fw[2][TN];
   uint32_t sa[TM], sw, nsa[TM], nsw;
+  float wsa[TM];                                   // WIDE: scales of the activations for widen8
   auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
   auto read_a = [&](int i, int ks) {
 #pragma unroll
@@ -415,16 +423,19 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = nsa[i] >> (8 * (t & 3));
     sw = nsw >> (8 * (t & 3));
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) wsa[i] = wide_row_scale(sa[i], sw);
+    }
   };
   constexpr int GS = TM * TN;
   auto product = [&](int ks, int set, int i, int j) {
     if constexpr (WIDE) {
-      // 8 of a lane's 32 values at a time, as bf16 with the block's scale (exact)
-      const float as = widen_scale(sa[i]), ws = widen_scale(sw);
+      // 8 of a lane's 32 values at a time, as bf16 with the blocks' scales (exact)
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const bf16x8 a = widen8(fa[i].v[2 * x], fa[i].v[2 * x + 1], as);
-        const bf16x8 w = widen8(fw[set][j].v[2 * x], fw[set][j].v[2 * x + 1], ws);
+        const bf16x8 a = widen8(fa[i].v[2 * x], fa[i].v[2 * x + 1], wsa[i]);
+        const bf16x8 w = widen8(fw[set][j].v[2 * x], fw[set][j].v[2 * x + 1], kWideWeightScale);
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, a, acc[i][j], 0, 0, 0);
       }
       fence();

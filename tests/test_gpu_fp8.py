@@ -741,3 +741,37 @@ def test_gemm_residual_of_long_sums_with_gates(torch, f3c, gated, M, N, K):
     got = _residual(torch, f3c, aq, ascl, wq, wscl, gate=gate)
     assert np.all(np.abs(got - want) <= (K / 16 + 16) * 2.0 ** -23 * tot + 2.0 ** -22 * np.abs(want))
     assert _rel(got, want) <= np.sqrt(K / 16 + 16) * 2.0 ** -23 + 2.0 ** -23
+
+
+@pytest.mark.parametrize("K", [272, 2064])
+def test_gemm_scales_at_their_ends(torch, f3c, K):
+    """A product knows its blocks' scales by their product alone: every pair of bytes that multiply to 1 gives the bits
+    of unit scales, from 2^-127 to 2^127."""
+    aq, _, wq, _, _ = _operands(40, 144, K, 3)
+    kb = -(-K // 128)
+    same = lambda e, n: np.full((n, kb), e, np.uint8)  # noqa: E731
+    want = _residual(torch, f3c, aq, same(127, 40), wq, same(127, 2))
+    assert np.isfinite(want).all() and np.abs(want).max() > 0
+    for e in (0, 1, 7, 8, 64, 119, 135, 200, 246, 247, 253, 254):
+        say("gemm_fp8 scale bytes", K, e)
+        assert np.array_equal(_residual(torch, f3c, aq, same(e, 40), wq, same(254 - e, 2)), want), e
+
+
+@pytest.mark.parametrize("K", [272, 2064])
+def test_gemm_single_products_at_any_scales(torch, f3c, K):
+    """Rows with one value that is not zero, under any two scale bytes: its products have at most 8 significant bits, so
+    that each is exact wherever float32 holds it, but for what lies below 2^-80."""
+    rng = np.random.default_rng(K)
+    M, N, kb = 3000, 144, -(-K // 128)
+    aq, ascl = np.zeros((M, K), np.uint8), rng.integers(0, 255, (M, kb), dtype=np.uint8)
+    code = lambda n: (rng.integers(0, 127, n) | rng.integers(0, 2, n) << 7).astype(np.uint8)  # noqa: E731
+    aq[np.arange(M), rng.integers(0, K, M)] = code(M)
+    aq[:200][aq[:200] != 0] = 0x7E                         # the largest value beside the smallest weights
+    wq, wscl = code(N * K).reshape(N, K), rng.integers(0, 255, (2, kb), dtype=np.uint8)
+    wq[::3] = wq[::3] & 0x80 | 1
+    want = fp8.linear(fp8.dequantise(aq, ascl), fp8.dequantise(wq, wscl, 128))
+    say("gemm_fp8 single products", K)
+    got = _residual(torch, f3c, aq, ascl, wq, wscl)
+    held = np.abs(want) < 2.0 ** 128
+    assert np.all(np.abs(got - want)[held] <= np.where(np.abs(want) < 2.0 ** -80, 2.0 ** -80, 0.0)[held])
+    assert held.mean() > 0.5 and (np.abs(want[held]) > 2.0 ** 100).any()
