@@ -655,8 +655,10 @@ constexpr Tile8Cost kTile8Cost[] = {
     {128, 128, 1, 1.730, 0.094, 0.237, 0.000, 0.377, 2.182, 0.000, 0.000, 0.971, 3.287, 1.046},
 };
 
-// The same for products on bf16 instructions, residual epilogue: a fit to 272 calls
-// with K = 4112 to 16384 whose pick is 0.2% from the best in the mean, 10% at worst.
+// The same for products on bf16 instructions (residual epilogue, K beyond 2048): a fit to
+// 272 calls with K = 4112 to 16384. It holds below as well: over 634 other calls with K =
+// 2064 to 16144, 239 of them up to 4096, its pick is 0.3% from the best in the mean, 18% at
+// worst (17606 x 544 x 14080), and a new fit over shorter K gains nothing.
 constexpr Tile8Cost kTile8WideCost[] = {
     {256, 256, 1, 0.000, 0.000, 2.263, 0.000, 0.341, 6.636, 0.000, 0.000, 0.000, 24.990, 0.000},
     {128, 128, 2, 0.000, 0.653, 0.359, 0.000, 0.532, 0.000, 0.000, 0.000, 0.000, 4.247, 0.000},
