@@ -286,24 +286,13 @@ hipError_t launch_resid_norm_w(ResidNormArgs a, int64_t rows, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Waves per row: of 512 columns (a lane's 8) up to 2048, of 1024 beyond, where the waves
-// of a row would be too many. A wave of half the columns holds half the registers and
-// has one less round of loads to wait for (us at 820 / 20000 rows, bf16 to 8 bits): width
-// 1024 in two waves of 512 5.2 / 38.7, in one of 1024 5.5 / 40.2; 1320 in three 6.1 / 51.6, in
-// two of 1024 6.4 / 53.4; 2048 in four 7.0 / 86.3, in two 7.3 / 92.4; but 2560 in five 7.9 / 120.7,
-// in three of 1024 8.2 / 119.6, and from float32 rows 7.8 / 157.7 against 7.8 / 148.9. Beyond
-// 4096 their number is even (width 4608 in six 15.3 / 245, in five 15.8 / 225; 7168 in eight 18.5
-// / 328, in seven 18.8 / 358). Six and eight waves from float32 rows to 8 bits spill 36
-// bytes a lane.
 template <typename TY, int OUT>
 hipError_t launch_resid_norm_t(const ResidNormArgs& a, int rows, hipStream_t s) {
-  switch ((a.d + 511) / 512) {
-    case 1: return launch_resid_norm_w<TY, OUT, 1, 1>(a, rows, s);
-    case 2: return launch_resid_norm_w<TY, OUT, 1, 2>(a, rows, s);
-    case 3: return launch_resid_norm_w<TY, OUT, 1, 3>(a, rows, s);
-    case 4: return launch_resid_norm_w<TY, OUT, 1, 4>(a, rows, s);
-  }
-  switch ((a.d + 1023) / 1024) {
+  if (a.d <= 512) return launch_resid_norm_w<TY, OUT, 1, 1>(a, rows, s);
+  if (a.d > 1024 && a.d <= 1536) return launch_resid_norm_w<TY, OUT, 1, 3>(a, rows, s);
+  switch ((a.d + 1023) / 1024) {                   // waves of 1024 columns
+    case 1: return launch_resid_norm_w<TY, OUT, 2, 1>(a, rows, s);
+    case 2: return launch_resid_norm_w<TY, OUT, 2, 2>(a, rows, s);
     case 3: return launch_resid_norm_w<TY, OUT, 2, 3>(a, rows, s);
     case 4: return launch_resid_norm_w<TY, OUT, 2, 4>(a, rows, s);
     case 5:
