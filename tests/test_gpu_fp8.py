@@ -775,3 +775,27 @@ def test_gemm_single_products_at_any_scales(torch, f3c, K):
     held = np.abs(want) < 2.0 ** 128
     assert np.all(np.abs(got - want)[held] <= np.where(np.abs(want) < 2.0 ** -80, 2.0 ** -80, 0.0)[held])
     assert held.mean() > 0.5 and (np.abs(want[held]) > 2.0 ** 100).any()
+
+
+@pytest.mark.parametrize("d", [512, 520, 1024, 1320, 2048, 2056, 4096, 4608, 8192])
+def test_resid_norm_rows_do_not_depend_on_their_number(torch, f3c, d):
+    """Of many rows a wave works off several in turn; each has the bits of a call of its own few, in every count of waves
+    per row."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    rows, off = 20000, [0, 7000, 7001, 20000]
+    h0, y, mod = r(rows, d), r(rows, d).to(torch.bfloat16), [r(3, d) for _ in range(3)]
+    w = [r(d), r(d)]
+
+    def run(lo, hi, off, b):
+        h, out = h0[lo:hi].clone(), torch.zeros(hi - lo, d, dtype=torch.uint8, device="cuda")
+        so = torch.zeros(hi - lo, f3c.fp8_scale_stride(d), dtype=torch.uint8, device="cuda")
+        say("resid_norm rows", d, lo, hi)
+        f3c.op_resid_norm(f3c.F3C_BF16, f3c.F3C_FP8, h, y=y[lo:hi], off=off, out=out, out_scale=so, post=f3c.F3C_NORM_RMS,
+                          pre=f3c.F3C_NORM_LAYER, post_w=w[0], pre_w=w[1], gate=mod[0][b], shift=mod[1][b], scale=mod[2][b])
+        return h, out, so
+
+    many = run(0, rows, off, slice(0, 3))
+    for lo, hi, b in ((0, 5, 0), (6990, 7000, 0), (7000, 7001, 1), (7001, 7100, 2), (13000, 13001, 2), (19990, 20000, 2)):
+        for x, z in zip(run(lo, hi, None, slice(b, b + 1)), many):
+            assert torch.equal(x, z[lo:hi]), (lo, hi)
