@@ -286,16 +286,17 @@ hipError_t launch_resid_norm_w(ResidNormArgs a, int64_t rows, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Waves per row: of 1024 columns, but of 512 (a lane's 8) up to 512 and from 1032 to 1536. With
-// half the columns a wave waits for half the loads and holds half the registers: faster
-// while a call's rows fit the last-level cache (256 MB). Beyond it more waves per row
-// read memory less well, unless the wave of 1024 that they replace is half empty. us at 9831 /
-// 65536 rows, bf16 to 8 bits: width 1024 in two of 512 21.6 / 164.1, in one of 1024 25.0 / 145.7;
-// 1320 in three 27.2 / 216.3, in two of 1024 32.9 / 219.1; 1536 29.9 / 237.9 against 35.0 / 237.8;
-// 2048 (at 32768 rows) in four 159.9, in two 155.0; 2560 (at 820 / 20000 rows, float32 to 8 bits)
-// in five 7.9 / 147.5, in three of 1024 7.8 / 140.4. Beyond 4096 the number is even: width 4608
-// (bf16, 820 / 20000 rows) in six 15.3 / 245, in five 15.8 / 225; 7168 in eight 18.5 / 328, in
-// seven 18.8 / 358 (five would be for many rows alone). Six and eight waves from float32 rows to 8 bits spill 36 bytes a lane.
+// Waves per row: of 1024 columns, but of 512 (a lane's 8) up to 512 and from 1032 to
+// 1536. With half the columns a wave waits for half the loads and holds half the
+// registers: faster while a call's rows fit the last-level cache (256 MB). Beyond it
+// more waves per row read memory less well, unless the wave of 1024 that they replace
+// is half empty. us at 9831 / 65536 rows, bf16 to 8 bits: width 1024 in two of 512 21.6 /
+// 164.1, in one of 1024 25.0 / 145.7; 1320 in three 27.2 / 216.3, in two of 1024 32.9 /
+// 219.1; 1536 29.9 / 237.9 against 35.0 / 237.8; 2048 (at 32768 rows) in four 159.9, in
+// two 155.0; 2560 (at 820 / 20000 rows, float32 to 8 bits) in five 7.9 / 147.5, in three
+// of 1024 7.8 / 140.4. Beyond 4096 the number is even: width 4608 (bf16, 820 / 20000 rows)
+// in six 15.3 / 245, in five 15.8 / 225 (few rows before many); 7168 in eight 18.5 / 328, in
+// seven 18.8 / 358. Six and eight waves from float32 rows to 8 bits spill 36 bytes a lane.
 template <typename TY, int OUT>
 hipError_t launch_resid_norm_t(const ResidNormArgs& a, int rows, hipStream_t s) {
   if (a.d <= 512) return launch_resid_norm_w<TY, OUT, 1, 1>(a, rows, s);

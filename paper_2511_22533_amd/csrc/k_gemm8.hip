@@ -195,8 +195,10 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
     gv[e] = g4.x, gv[e + 1] = g4.y, gv[e + 2] = g4.z, gv[e + 3] = g4.w;
   }
   // Residual rows are read 32 rows ahead of their update, but where four workgroups
-  // share the registers (32768 x 1024 x 4096 in 256 x 256 tiles 175.6 -> 173.4 us, 820
-  // rows in 64 x 128 17.3 -> 16.3; four of 128 x 128 would spill: 186 -> 215).
+  // share the registers: 9831 x 1024 x 1024 25.6 -> 24.9 us, 9831 x 1024 x 2048 34.3 -> 33.7,
+  // others as without (32768 x 1024 x 2048 90.8 / 91.8, 820 rows 7.6 / 7.7); four of 128 x 128
+  // would spill: 32768 x 1024 x 1024 60.9 -> 82.6. The 256 x 256 tile spills 20 bytes a lane
+  // here, behind its loop.
   constexpr int T = 32 / RPI;
   constexpr bool kAhead = OCC < 4;
   float4 hb[2][EPI == EPI_RESID ? T : 1];
@@ -516,6 +518,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
     for (int q = 0; q < DT; ++q)
       if (s < STAGES - 1 || q < EARLY) fetch1(q, min(s, KT - 1), s);
   }
+  // (what stands for the first stage alone; ahead of the first product the compiler waits
+  // for the bias, and with it for every stage in flight)
   wait_vm<(STAGES - 2) * DT + EARLY>();
   __syncthreads();
   // (in the loop's order, so that the compiler's waits in it are exact)

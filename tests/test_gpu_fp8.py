@@ -799,3 +799,20 @@ def test_resid_norm_rows_do_not_depend_on_their_number(torch, f3c, d):
     for lo, hi, b in ((0, 5, 0), (6990, 7000, 0), (7000, 7001, 1), (7001, 7100, 2), (13000, 13001, 2), (19990, 20000, 2)):
         for x, z in zip(run(lo, hi, None, slice(b, b + 1)), many):
             assert torch.equal(x, z[lo:hi]), (lo, hi)
+
+
+@pytest.mark.parametrize("K", [400, 2064])
+def test_gemm_bad_scales_stay_alone(torch, f3c, K):
+    """A NaN scale of a row is NaN in its row, one of a block of weights in the block's columns, on either path."""
+    aq, ascl, wq, wscl, _ = _operands(50, 272, K, 8)
+    good = _residual(torch, f3c, aq, ascl, wq, wscl)
+    ascl[20, 1], wscl[1, 3] = 255, 255
+    aq[:, 128 * 3:] = 0                                  # (0 times NaN is NaN as well)
+    say("gemm_fp8 NaN scales", K)
+    got = _residual(torch, f3c, aq, ascl, wq, wscl)
+    bad = np.zeros(good.shape, bool)
+    bad[20], bad[:, 128:256] = True, True
+    assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
+    wscl[1, 3] = 127
+    again = _residual(torch, f3c, aq, ascl, wq, wscl)
+    assert np.array_equal(got[~bad], again[~bad])
