@@ -279,14 +279,19 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // from registers, sustain 3.5 to 3.8 PFLOP/s (4.9 on zeros); 8192 x 8192 x 8192 takes
 // 410 to 470 us by box (2.7 to 2.35 PFLOP/s) at a clock of 1.6 GHz with the matrix
 // pipes busy 69% of the cycles. 256 x 256 tiles read LDS least (16-byte K halves of a
-// row as stages cost 10%: lines travel twice). Short K: the epilogue beside it, mostly
-// GELU's exponential and reciprocal, which only another workgroup's products can hide:
-// at 32768 x 4096 x 1024 into 8 bits one 256 x 256 workgroup per CU takes 175 us, four
-// of 128 x 128 in a single stage 157. Into a residual it is its 268 MB. Few rows: the
-// chain of K tiles, 0.2 to 0.3 us each, of LDS reads and two dependent products.
+// row as stages cost 10%: lines travel twice). Short K: no pipe alone; what one workgroup
+// waits for (its stage, GELU's exponential and reciprocal, its stores) another's
+// products have to hide. At 32768 x 4096 x 1024 into 8 bits matrix pipes and vector issue
+// are busy 43% of the cycles each and LDS reads 32%; one 256 x 256 workgroup per CU takes
+// 175 us, four of 128 x 128 in a single stage 157. On bf16 instructions (32768 x 1024 x
+// 4096 into the residual, 232 us) matrix pipes 57%, vector issue 40%, most of it the
+// widening. Few rows: the chain of K tiles, 0.2 to 0.5 us each, of LDS reads and dependent
+// products, with every pipe below a quarter (820 x 1024 x 4096: on the 208 CUs that have a
+// tile matrix 14%, vector issue 22%, LDS reads 8%).
 // Against the bf16 projections on one box (us, bf16 / here): 32768 x 4096 x 1024 GELU
-// 297 / 157 (out in 8 bits), 32768 x 1024 x 4096 gated residual 266 / 151, 9831 x 2048
-// x 1024 55 / 29, 9831 x 1024 x 4096 gated residual 93 / 50, of 820 rows 19 / 12.
+// 300 / 161 (out in 8 bits), 9831 x 2048 x 1024 55 / 29, 9831 x 1024 x 1024 gated residual 35 / 26;
+// on exact products, gated residual: 32768 x 1024 x 4096 271 / 232, 9831 rows 91 / 86, 820 rows
+// 18.6 / 18.7.
 template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, bool WIDE = false>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
@@ -642,7 +647,7 @@ hipError_t launch_dma(const Gemm8Args& a0, hipStream_t s) {
 // rows, every epilogue), each tile where it is within 2.5 times of the best, larger
 // calls weighing a little more: the pick is 0.5% slower than the best of eleven
 // measured tiles in the mean, 25% at worst; for calls over 17 GFLOP 1.1% (with neither
-// 192 x 256 nor 128 x 256 it was 5%: 9831 x 1024 x 4096 56.6 -> 49.7 us).
+// 192 x 256 nor 128 x 256 it was 5%: 9831 x 1024 x 4096 stored 48.1 -> 43.8 us).
 struct Tile8Cost {
   int bm, bn, per_cu;
   double fixed, k, k_round, k_group, k_load, round, group, load_store, load_gelu, load_resid, load_fp8;
