@@ -418,7 +418,8 @@ int f3c_op_quant_fp8(int32_t dtype, int32_t block_rows, int32_t rows, int32_t K,
  * of its size where the operands are normally distributed and by 2.1e-5 where A
  * holds GELU's outputs, and the residual by as much of gate * v. Into the residual,
  * sums of K > 2048 are formed from exact products on bf16 instructions instead, at
- * half the rate (1.4e-7). No gate is a gate of ones, bit for bit. N and K multiples of 16, M and N below 2^30, ceil(M/32) *
+ * half the rate (1.4e-7; products under 2^-81 may be lost). No gate is a gate of
+ * ones, bit for bit. N and K multiples of 16, M and N below 2^30, ceil(M/32) *
  * ceil(N/64) below 2^24 - 1; rows of A, W, out and resid 16-byte aligned, of bias
  * and gate too; lda, ldw, ldsa, ldsw below 2^22. The result of an output row does
  * not depend on M or on other rows, nor on scheduling. out, out_scale and resid

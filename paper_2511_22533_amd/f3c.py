@@ -662,8 +662,8 @@ def op_resid_norm(dtype: int, out_dtype: int, h, y=None, off=None, out=None, out
                   pre: int = F3C_NORM_LAYER, post_w=None, pre_w=None, gate=None, resid_scale: float = 1.0, shift=None,
                   scale=None, eps: float = 1e-6, stream=None):
     """The pass between two blocks: h += resid_scale * gate * (post(y) * post_w), out = (pre(h) * pre_w) * (1 + scale)
-    + shift. off: row offsets of the samples (default: one sample of all rows); gate, shift, scale: all that are given [B][d]
-    with one row stride, or all [d] for every sample. y None: the norm alone; out None: the update alone."""
+    + shift. off: row offsets of the samples (default: one sample of all rows); gate, shift, scale: all that are given
+    [B][d] with one row stride, or all [d] for every sample. y None: the norm alone; out None: the update alone."""
     T = _dtypes()
     if dtype not in (F3C_F32, F3C_BF16) or out_dtype not in (F3C_F32, F3C_BF16, F3C_FP8) or h.dim() != 2:
         raise ValueError("rows h, dtype F3C_F32 or F3C_BF16, out_dtype F3C_F32, F3C_BF16 or F3C_FP8 expected")
