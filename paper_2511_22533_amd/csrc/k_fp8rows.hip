@@ -2,7 +2,7 @@
 // the pass between two blocks (norm of the block's output, gated and scaled
 // residual update, norm and modulation of the next block's input). All of them
 // read and write HBM once and are bound by it (a 1 GiB copy moves 4.8 to 5.3 TB/s by
-// box). On one box, with a copy of 4.8: quantisation of 32768 x 4096 bf16 rows 79 us, 5.1
+// card). On one, with a copy of 4.8: quantisation of 32768 x 4096 bf16 rows 79 us, 5.1
 // TB/s, of a 16384 x 8192 bf16 weight 78 us, 5.1; the pass between blocks over 32768 x 1024
 // bf16 to 8 bits 77 us, 4.8, with as much written as read. Under some 20 MB the 1.9 us of a
 // launch and one or more trips to memory count as much: 9831 x 1024 quantised 5.8 us (6.9

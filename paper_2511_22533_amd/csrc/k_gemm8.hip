@@ -277,7 +277,7 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 //
 // What bounds it. Long K, many rows: power. On such operands the matrix cores alone,
 // from registers, sustain 3.5 to 3.8 PFLOP/s (4.9 on zeros); 8192 x 8192 x 8192 takes
-// 410 to 470 us by box (2.7 to 2.35 PFLOP/s) at a clock of 1.6 GHz with the matrix
+// 410 to 470 us by card (2.7 to 2.35 PFLOP/s) at a clock of 1.6 GHz with the matrix
 // pipes busy 69% of the cycles. 256 x 256 tiles read LDS least (16-byte K halves of a
 // row as stages cost 10%: lines travel twice). Short K: no pipe alone; what one workgroup
 // waits for (its stage, GELU's exponential and reciprocal, its stores) another's
@@ -288,7 +288,7 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // widening. Few rows: the chain of K tiles, 0.2 to 0.5 us each, of LDS reads and dependent
 // products, with every pipe below a quarter (820 x 1024 x 4096: on the 208 CUs that have a
 // tile matrix 14%, vector issue 22%, LDS reads 8%).
-// Against the bf16 projections on one box (us, bf16 / here): 32768 x 4096 x 1024 GELU
+// Against the bf16 projections on one card (us, bf16 / here): 32768 x 4096 x 1024 GELU
 // 300 / 161 (out in 8 bits), 9831 x 2048 x 1024 55 / 29, 9831 x 1024 x 1024 gated residual 35 / 26;
 // on exact products, gated residual: 32768 x 1024 x 4096 271 / 232, 9831 rows 91 / 86, 820 rows
 // 18.6 / 18.7.
