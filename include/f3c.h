@@ -54,6 +54,7 @@ extern "C" {
 #define F3C_F32 0         /* float32 compute (debug / small models) */
 #define F3C_BF16 1        /* bfloat16 operands, float32 accumulation and residual */
 #define F3C_FP8 2         /* e4m3 rows with power-of-two scales (operators only, not a model dtype) */
+#define F3C_I8 3          /* 8-bit integer rows with a float32 scale each (operators only) */
 
 #define F3C_MAX_BATCH 64
 #define F3C_STATE_GUIDED 1u   /* state flag: room for guided steps (two passes per sample) */
@@ -428,6 +429,88 @@ int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const voi
                     const void* A_scale, int32_t ldsa, const void* W, int32_t ldw, const void* W_scale, int32_t ldsw,
                     const float* bias, const float* gate, void* out, int32_t ldo, void* out_scale, int32_t ldso,
                     float* resid, int32_t ldr, f3c_stream stream);
+
+/* 8-bit integer rows (F3C_I8): whole numbers -127..127 with one float32 scale for
+ * each row, a token's for activations and an output channel's for weights; scales
+ * float32 [rows], 4-byte aligned.
+ *
+ * Quantisation of x [rows][ldx] (dtype F3C_F32 or F3C_BF16) to q int8 [rows][ldq]:
+ * scale = max|x| / 127 rounded to float32, at least 2^-126; q = the whole number
+ * nearest to x / scale (the real quotient), ties to even. A row that holds a NaN or an
+ * infinity gets the scale NaN and zeros, so that its row (column) of a product is NaN.
+ * K a multiple of 8, below 2^30; x and q rows 16- and 8-byte aligned; fewer than 2^24
+ * rows. Errors: F3C_EINVAL (dtype, shape, leading dims, NULL or misaligned pointers). */
+int f3c_op_quant_i8(int32_t dtype, int32_t rows, int32_t K, const void* x, int32_t ldx, void* q, int32_t ldq,
+                    float* scale, f3c_stream stream);
+
+/* f3c_op_gemm on 8-bit integers: v[m][n] = A_scale[m] * (W_scale[n] * S) + bias[n] with S
+ * = sum over k of A[m][k] * W[n][k], exact (int32), A int8 [M][lda], W int8 [N][ldw],
+ * bias f32 [N] or NULL; S in float32 and the two products and the sum are rounded one by
+ * one. epilogue 0: out bf16 [M][ldo] = v; 1: out bf16 = GELU_tanh(v); 2: resid f32 [M][ldr]
+ * += (gate ? gate[n] : 1) * v. N and K multiples of 16, K at most 133120, M and N below
+ * 2^30, ceil(M/32) * ceil(N/64) below 2^24 - 1; rows of A, W, out and resid, bias and gate
+ * 16-byte aligned; lda and ldw below 2^22. Values of -128 are taken as they are (K then at
+ * most 131056). The result of an output row does not depend on M or on other rows, nor on
+ * scheduling. out and resid must not overlap the operands. Errors: F3C_EINVAL. */
+int f3c_op_gemm_i8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,
+                   const float* A_scale, const void* W, int32_t ldw, const float* W_scale, const float* bias,
+                   const float* gate, void* out, int32_t ldo, float* resid, int32_t ldr, f3c_stream stream);
+
+/* Keys and values held in 8 bits, for instance the condition's, which every step and
+ * block of a trajectory reads again, or those of the tokens that a sequence holds so far:
+ * a pool of pages of F3C_PAGE_TOKENS tokens, each page with a tile of K and one of V for
+ * every key head, e4m3 with one power-of-two scale a tile (an E8M0 byte, as F3C_FP8's
+ * blocks). Tile of K: [64 tokens][head_dim]; of V: [head_dim][64], token 16t + 4c + e (c, e
+ * < 4) of the page at 16c + 4t + e. table names each sample's pages in order (device; it
+ * may change between calls); samples may share pages that are no longer written. An
+ * entry outside [0, n_pages) is no page: nothing is written to it, and attention passes
+ * its tokens over. All pointers are device memory, k and v 16-byte aligned, table
+ * 4-byte. The tiles' bytes behind a sample's last token are neither written nor used. */
+#define F3C_PAGE_TOKENS 64
+typedef struct {
+  int32_t kv_heads;         /* 1..1024 */
+  int32_t head_dim;         /* 32, 64 or 128 */
+  int32_t n_pages;          /* of the pool */
+  int32_t max_pages;        /* entries of a sample's row of table */
+  void* k;                  /* e4m3 [n_pages][kv_heads][64 * head_dim] */
+  void* v;
+  void* k_scale;            /* E8M0 [n_pages][kv_heads] */
+  void* v_scale;
+  const int32_t* table;     /* [batch][max_pages] */
+} f3c_cache8;
+
+/* Appends rows off[b]..off[b+1] (B+1 non-decreasing host ints) of k [.][ldk] and v
+ * [.][ldv] (dtype F3C_F32 or F3C_BF16, key head h at columns h * head_dim) to sample b's
+ * tokens, of which its pages hold len[b] (B host ints): they become tokens len[b]... A
+ * tile's scale is the smallest 2^e, e in [-126, 127], that keeps its finite values within
+ * 448 * 2^e, and not below what it was if the tile holds tokens of before: where the new
+ * ones need a larger one, those are rounded anew (exact but for e4m3's subnormals, whose
+ * step is then the larger scale's). NaN and infinities become NaN and do not count for the
+ * scale. The pages that one call writes must be distinct, else what they hold is
+ * unspecified. Rows 16-byte aligned; len[b] + new rows at most 64 * max_pages; fewer than
+ * 2^23 tiles written in all. Errors: F3C_EINVAL. */
+int f3c_op_cache8_append(const f3c_cache8* cache, int32_t dtype, int32_t batch, const int32_t* len_host,
+                         const int32_t* off_host, const void* k, int32_t ldk, const void* v, int32_t ldv,
+                         f3c_stream stream);
+
+/* Attention over it, f3c_op_attention's on bf16 rows: queries q_off[b]..q_off[b+1] of q
+ * [.][ldq] and their outputs o [.][ldo] (heads * head_dim columns; query head h reads key
+ * head h / (heads / kv_heads)) over the len[b] tokens of sample b; o = softmax(q K^T /
+ * sqrt(head_dim)) V. causal: a sample's queries are its last tokens, query i of n seeing
+ * tokens 0..len - n + i. A query that sees no token gets zeros. q_prescaled as in
+ * f3c_op_attention. Any finite scores; tiles' values between 2^-100 and 2^100 in
+ * magnitude. NaN in a token reaches the queries that see it and no others. workspace
+ * (device, 16-byte aligned, may be NULL): the key range is split over workgroups where
+ * there are few queries, as far as the workspace holds the splits' results;
+ * f3c_op_cache8_attention_bytes says how much the call makes use of (it looks at no device
+ * memory: pointers may be NULL). Rows of q 16-byte aligned, of o 8-byte. ceil(queries * heads /
+ * kv_heads / 16) * kv_heads summed over samples below 2^22; heads at most 65535.
+ * Errors: F3C_EINVAL. */
+int f3c_op_cache8_attention_bytes(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,
+                                  const int32_t* len_host, int32_t causal, size_t* bytes);
+int f3c_op_cache8_attention(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,
+                            const int32_t* len_host, const void* q, int32_t ldq, void* o, int32_t ldo, int32_t causal,
+                            int32_t q_prescaled, void* workspace, size_t workspace_bytes, f3c_stream stream);
 
 #define F3C_NORM_NONE 0
 #define F3C_NORM_LAYER 1  /* (x - mean) / sqrt(var + eps), var over the row, biased */

@@ -21,7 +21,8 @@ LIB = os.path.join(LIB_DIR, "libf3c.so")
 DRIVER = os.path.join(LIB_DIR, "f3c_drive")
 ROOT = os.path.dirname(HERE)
 
-SOURCES = ["k_select.hip", "k_rows.hip", "k_gemm.hip", "k_gemm8.hip", "k_fp8rows.hip", "k_attn.hip", "k_occupancy.hip", "f3c.cpp"]
+SOURCES = ["k_select.hip", "k_rows.hip", "k_gemm.hip", "k_gemm8.hip", "k_fp8rows.hip", "k_i8rows.hip", "k_cache8.hip", "k_attn.hip",
+           "k_occupancy.hip", "f3c.cpp"]
 DRIVER_SOURCE = "f3c_drive.hip"
 
 FLAGS = [

@@ -18,6 +18,7 @@
 #include "../../include/f3c.h"
 #include "common.h"
 #include "kernels.h"
+#include "cache8.h"
 #include "kernels8.h"
 
 using namespace f3c;
@@ -1123,6 +1124,140 @@ int f3c_op_gemm_fp8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const voi
     if (int rc = check_scales("out_scale", out_scale, ldso, N, M)) return rc;
   HIP_TRY(launch_gemm_fp8(epilogue, M, N, K, A, lda, A_scale, ldsa, W, ldw, W_scale, ldsw, bias, gate, out, ldo,
                           out_scale, ldso, resid, ldr, (hipStream_t)stream));
+  return F3C_OK;
+}
+
+int f3c_op_quant_i8(int32_t dtype, int32_t rows, int32_t K, const void* x, int32_t ldx, void* q, int32_t ldq,
+                    float* scale, f3c_stream stream) {
+  if (dtype != F3C_F32 && dtype != F3C_BF16) return fail(F3C_EINVAL, "bad dtype");
+  if (rows < 0 || rows >= (1 << 24) || K <= 0 || K % 8 || K >= (1 << 30))
+    return fail(F3C_EINVAL, "bad shape (fewer than 2^24 rows, K a multiple of 8, below 2^30)");
+  if (rows && (!x || !q || !scale)) return fail(F3C_EINVAL, "NULL argument");
+  if (ldx < K || ldq < K || !aligned_rows(x, ldx, dtype == F3C_BF16 ? 2 : 4, 16) || !aligned_rows(q, ldq, 1, 8))
+    return fail(F3C_EINVAL, "bad leading dims or alignment (x rows 16 bytes, q rows 8)");
+  if ((uintptr_t)scale % 4) return fail(F3C_EINVAL, "scale must be 4-byte aligned");
+  HIP_TRY(launch_quant_i8(dtype, rows, K, x, ldx, q, ldq, scale, (hipStream_t)stream));
+  return F3C_OK;
+}
+
+int f3c_op_gemm_i8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* A, int32_t lda,
+                   const float* A_scale, const void* W, int32_t ldw, const float* W_scale, const float* bias,
+                   const float* gate, void* out, int32_t ldo, float* resid, int32_t ldr, f3c_stream stream) {
+  if (epilogue < EPI_STORE || epilogue > EPI_RESID) return fail(F3C_EINVAL, "bad epilogue");
+  if (M < 0 || N <= 0 || K <= 0 || M >= (1 << 30) || N >= (1 << 30)) return fail(F3C_EINVAL, "bad shape");
+  if (K > kI8MaxK) return fail(F3C_EINVAL, "K above %d: sums of products of 8-bit integers leave 32 bits", kI8MaxK);
+  if ((int64_t)((M + 31) / 32) * ((N + 63) / 64) >= (1 << 24) - 1)
+    return fail(F3C_EINVAL, "too many outputs for one launch");
+  if (N % 16 || K % 16) return fail(F3C_EINVAL, "N and K must be multiples of 16");
+  if ((M && (!A || !A_scale)) || !W || !W_scale) return fail(F3C_EINVAL, "NULL operand or scales");
+  if (lda < K || ldw < K || !aligned_rows(A, lda, 1, 16) || !aligned_rows(W, ldw, 1, 16) || lda >= (1 << 22) ||
+      ldw >= (1 << 22))
+    return fail(F3C_EINVAL, "bad leading dims or alignment of A or W (rows below 2^22 bytes)");
+  if ((uintptr_t)A_scale % 4 || (uintptr_t)W_scale % 4) return fail(F3C_EINVAL, "scales must be 4-byte aligned");
+  if ((bias && (uintptr_t)bias % 16) || (gate && (uintptr_t)gate % 16))
+    return fail(F3C_EINVAL, "bias and gate must be 16-byte aligned");
+  if (gate && epilogue != EPI_RESID) return fail(F3C_EINVAL, "gate goes with the residual epilogue");
+  if (epilogue == EPI_RESID ? ((M && !resid) || ldr < N || !aligned_rows(resid, ldr, 4, 16))
+                            : ((M && !out) || ldo < N || !aligned_rows(out, ldo, 2, 16)))
+    return fail(F3C_EINVAL, "bad output (NULL, leading dim below N or rows not 16-byte aligned)");
+  HIP_TRY(launch_gemm_i8(epilogue, M, N, K, A, lda, A_scale, W, ldw, W_scale, bias, gate, out, ldo, resid, ldr,
+                         (hipStream_t)stream));
+  return F3C_OK;
+}
+
+// A cache's sizes, the samples' rows and the tokens that their pages hold (up to `extra`
+// more with a sample's rows).
+static int check_cache8(const f3c_cache8* cache, int32_t batch, const int32_t* off_host, const int32_t* len_host,
+                        bool append, Cache8* c, Segs* rows, Lens* len) {
+  if (!cache || !off_host || !len_host) return fail(F3C_EINVAL, "NULL argument");
+  if (cache->head_dim != 32 && cache->head_dim != 64 && cache->head_dim != 128)
+    return fail(F3C_EINVAL, "head_dim must be 32, 64 or 128");
+  if (cache->kv_heads < 1 || cache->kv_heads > 1024 || cache->n_pages < 0 || cache->max_pages < 0 ||
+      cache->max_pages > (1 << 24))
+    return fail(F3C_EINVAL, "bad sizes of the cache");
+  if (int rc = segs_from_host(batch, off_host, 0x7fffffff, rows)) return rc;
+  for (int b = 0; b < batch; ++b) {
+    len->n[b] = len_host[b];
+    const int64_t n = (int64_t)len_host[b] + (append ? rows->off[b + 1] - rows->off[b] : 0);
+    if (len_host[b] < 0 || n > (int64_t)cache->max_pages * kPage)
+      return fail(F3C_EINVAL, "sample %d: its tokens do not fit its row of the table", b);
+  }
+  *c = Cache8{(uint8_t*)cache->k, (uint8_t*)cache->v, (uint8_t*)cache->k_scale, (uint8_t*)cache->v_scale,
+              cache->table, cache->kv_heads, cache->head_dim, cache->n_pages, cache->max_pages};
+  return F3C_OK;
+}
+
+static int check_cache8_memory(const f3c_cache8* c) {
+  if (c->n_pages && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return fail(F3C_EINVAL, "NULL pages or scales");
+  if (c->max_pages && !c->table) return fail(F3C_EINVAL, "NULL table");
+  if ((uintptr_t)c->k % 16 || (uintptr_t)c->v % 16 || (uintptr_t)c->table % 4)
+    return fail(F3C_EINVAL, "pages must be 16-byte aligned, the table 4-byte");
+  return F3C_OK;
+}
+
+int f3c_op_cache8_append(const f3c_cache8* cache, int32_t dtype, int32_t batch, const int32_t* len_host,
+                         const int32_t* off_host, const void* k, int32_t ldk, const void* v, int32_t ldv,
+                         f3c_stream stream) {
+  if (dtype != F3C_F32 && dtype != F3C_BF16) return fail(F3C_EINVAL, "bad dtype");
+  Cache8 c;
+  Segs rows;
+  Lens len;
+  if (int rc = check_cache8(cache, batch, off_host, len_host, true, &c, &rows, &len)) return rc;
+  if (int rc = check_cache8_memory(cache)) return rc;
+  const int w = c.kv_heads * c.hd, es = dtype == F3C_BF16 ? 2 : 4;
+  if (rows.off[batch] > rows.off[0] && (!k || !v)) return fail(F3C_EINVAL, "NULL argument");
+  if (ldk < w || ldv < w || !aligned_rows(k, ldk, es, 16) || !aligned_rows(v, ldv, es, 16))
+    return fail(F3C_EINVAL, "bad leading dims or alignment (rows 16 bytes)");
+  int64_t tiles = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = rows.off[b + 1] - rows.off[b];
+    if (n) tiles += (len.n[b] + n + kPage - 1) / kPage - len.n[b] / kPage;
+  }
+  if (tiles * c.kv_heads * 2 >= (1 << 23)) return fail(F3C_EINVAL, "too many tiles for one launch");
+  HIP_TRY(launch_cache8_append(c, dtype, len, rows, k, ldk, v, ldv, (hipStream_t)stream));
+  return F3C_OK;
+}
+
+// What both calls of the attention look at.
+static int check_cache8_attention(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,
+                                  const int32_t* len_host, int32_t causal, Cache8* c, Segs* rows, Lens* len) {
+  if (int rc = check_cache8(cache, batch, q_off_host, len_host, false, c, rows, len)) return rc;
+  if (heads < 1 || heads > 65535 || heads % c->kv_heads)
+    return fail(F3C_EINVAL, "heads must be a multiple of kv_heads, at most 65535");
+  if (causal != 0 && causal != 1) return fail(F3C_EINVAL, "causal must be 0 or 1");
+  int64_t tiles = 0;
+  for (int b = 0; b < batch; ++b)
+    tiles += ((int64_t)(rows->off[b + 1] - rows->off[b]) * (heads / c->kv_heads) + 15) / 16;
+  if (tiles * c->kv_heads >= (1 << 22)) return fail(F3C_EINVAL, "too many queries for one launch");
+  return F3C_OK;
+}
+
+int f3c_op_cache8_attention_bytes(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,
+                                  const int32_t* len_host, int32_t causal, size_t* bytes) {
+  Cache8 c;
+  Segs rows;
+  Lens len;
+  if (!bytes) return fail(F3C_EINVAL, "NULL argument");
+  if (int rc = check_cache8_attention(cache, heads, batch, q_off_host, len_host, causal, &c, &rows, &len)) return rc;
+  *bytes = cache8_attention_bytes(c, heads, rows, len, causal);
+  return F3C_OK;
+}
+
+int f3c_op_cache8_attention(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,
+                            const int32_t* len_host, const void* q, int32_t ldq, void* o, int32_t ldo, int32_t causal,
+                            int32_t q_prescaled, void* workspace, size_t workspace_bytes, f3c_stream stream) {
+  Cache8 c;
+  Segs rows;
+  Lens len;
+  if (int rc = check_cache8_attention(cache, heads, batch, q_off_host, len_host, causal, &c, &rows, &len)) return rc;
+  if (int rc = check_cache8_memory(cache)) return rc;
+  if (q_prescaled != 0 && q_prescaled != 1) return fail(F3C_EINVAL, "q_prescaled must be 0 or 1");
+  if (rows.off[batch] > rows.off[0] && (!q || !o)) return fail(F3C_EINVAL, "NULL argument");
+  if (ldq < heads * c.hd || ldo < heads * c.hd || !aligned_rows(q, ldq, 2, 16) || !aligned_rows(o, ldo, 2, 8))
+    return fail(F3C_EINVAL, "bad leading dims or alignment (q rows 16 bytes, o rows 8)");
+  if ((uintptr_t)workspace % 16) return fail(F3C_EINVAL, "workspace must be 16-byte aligned");
+  HIP_TRY(launch_cache8_attention(c, heads, rows, len, q, ldq, o, ldo, causal, q_prescaled, workspace,
+                                  workspace ? workspace_bytes : 0, (hipStream_t)stream));
   return F3C_OK;
 }
 

@@ -49,6 +49,15 @@ struct Gemm8Args {
   int xq;                             // column groups of the XCD tile partition
 };
 
+// What the operands hold: e4m3 multiplied on the scaled 8-bit instructions, or
+// exactly on bf16 ones; or 8-bit integers (sa and sw are then float32, one for each
+// row of A and of W).
+enum Operands { OPS_FP8, OPS_FP8_WIDE, OPS_I8 };
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+template <int OPS> using Acc = std::conditional_t<OPS == OPS_I8, i32x16, f32x16>;
+
 // GELU in its tanh form as x / (1 + 2^(x (a + b x^2))), a = -2 log2(e) sqrt(2/pi),
 // b = 0.044715 a: five operations, an exponential and a reciprocal.
 __device__ __forceinline__ float gelu_fast(float x) {
@@ -82,9 +91,11 @@ __device__ __forceinline__ float wide_row_scale(uint32_t sa, uint32_t sw) {
 // holds four columns here and there of one row; rows leave in whole pieces). The
 // region is the wave's own and LDS operations of a wave keep their order. All of
 // the workgroup's LDS is free to use.
-template <int TM, int TN, int WTM, int WTN, int BM, int BN, int WGN, int OCC, int BYTES, int EPI>
-__device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)[TM][TN], char* lds, int m0, int n0,
-                                               int wm, int wn, int lane) {
+// Integer sums S become v = sa[m] (sw[n] S) + bias[n] as they leave LDS, where a lane's
+// columns are the same for all its rows; sa, sw and bias lie at `factors` in LDS.
+template <int TM, int TN, int WTM, int WTN, int BM, int BN, int WGN, int OCC, int BYTES, int EPI, int OPS>
+__device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, Acc<OPS> (&acc)[TM][TN], char* lds, int m0, int n0,
+                                               int wm, int wn, int lane, const float* factors) {
   const int g = lane >> 5, r32 = lane & 31, wave = wm * WGN + wn;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   constexpr int NW = (BM / WTM) * WGN;
@@ -181,7 +192,8 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
   } else {
   constexpr int RS = WTN * 4 + 16;
   static_assert(NW * 32 * RS <= BYTES, "epilogue buffer");
-  typedef __attribute__((address_space(3))) f32x4 lds_f4;
+  typedef std::conditional_t<OPS == OPS_I8, i32x4, f32x4> Four;
+  typedef __attribute__((address_space(3))) Four lds_f4;
   const uint32_t eb = lds0 + (uint32_t)(wave * 32 * RS);
   // columns per lane, lanes per row, rows per pass
   constexpr int VC = EPI == EPI_RESID ? 4 : 8, LPR = WTN / VC, RPI = 64 / LPR;
@@ -193,6 +205,14 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
     float4 g4 = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
     if (EPI == EPI_RESID && p.gate && in) g4 = *reinterpret_cast<const float4*>(p.gate + ecol + e);
     gv[e] = g4.x, gv[e + 1] = g4.y, gv[e + 2] = g4.z, gv[e + 3] = g4.w;
+  }
+  float col_scale[VC], col_bias[VC];
+  if constexpr (OPS == OPS_I8) {
+#pragma unroll
+    for (int e = 0; e < VC; ++e) {
+      col_scale[e] = factors[BM + ecol - n0 + e];
+      col_bias[e] = factors[BM + BN + ecol - n0 + e];
+    }
   }
   // Residual rows are read 32 rows ahead of their update, but where four workgroups
   // share the registers: 9831 x 1024 x 1024 25.6 -> 24.9 us, 9831 x 1024 x 2048 34.3 -> 33.7,
@@ -220,20 +240,26 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         *(lds_f4*)(uintptr_t)(eb + (uint32_t)(r32 * RS + (j * 32 + 8 * q + 4 * g) * 4)) =
-            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            Four{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (kAhead ? i + 1 < TM : true) load_h(kAhead ? i + 1 : i);   // (into the registers of what has just been written)
     const int row0 = m0 + wm * WTM + i * 32 + lane / LPR;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int row = row0 + t * RPI;
-      float v[VC];
+      float v[VC], row_scale;
+      if constexpr (OPS == OPS_I8) row_scale = factors[row - m0];
 #pragma unroll
       for (int e = 0; e < VC; e += 4) {
         const uint32_t at = eb + (uint32_t)((t * RPI + lane / LPR) * RS + ((lane % LPR) * VC + e) * 4);
-        const f32x4 c4 = *(lds_f4*)(uintptr_t)at;
+        const Four c4 = *(lds_f4*)(uintptr_t)at;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) v[e + x] = c4[x];
+        for (int x = 0; x < 4; ++x) {
+          if constexpr (OPS == OPS_I8)
+            v[e + x] = row_scale * (col_scale[e + x] * (float)c4[x]) + col_bias[e + x];
+          else
+            v[e + x] = c4[x];
+        }
       }
       if (row >= p.M || !in) continue;
       if constexpr (EPI == EPI_RESID) {
@@ -292,12 +318,13 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, f32x16 (&acc)
 // 300 / 161 (out in 8 bits), 9831 x 2048 x 1024 55 / 29, 9831 x 1024 x 1024 gated residual 35 / 26;
 // on exact products, gated residual: 32768 x 1024 x 4096 271 / 232, 9831 rows 91 / 86, 820 rows
 // 18.6 / 18.7.
-template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, bool WIDE = false>
+template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, int OPS = OPS_FP8>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
   constexpr int KTB = 128, ABUF = BM * KTB, SBUF = (BM + BN) * KTB;
   constexpr int DA = BM / 8, DB = BN / 8, DQ = (DA + DB) / NW;         // DMA blocks of 8 rows
-  constexpr int SA = (BM + 63) / 64, SX = (SA + NW) / NW;              // scale DMAs of A; all, per wave
+  constexpr bool WIDE = OPS == OPS_FP8_WIDE, I8 = OPS == OPS_I8;
+  constexpr int SA = (BM + 63) / 64, SX = I8 ? 0 : (SA + NW) / NW;     // scale DMAs of A; all, per wave
   constexpr int DT = DQ + SX;                                          // a wave's DMA instructions per K tile
   constexpr int SSET = 64 * NW * SX * 4;                               // bytes of a stage's scales
   static_assert(DA % NW == 0 && DB % NW == 0, "whole DMA blocks per wave");
@@ -305,7 +332,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   static_assert(STAGES > 1 || TM * TN > 2, "a single stage is refilled between the products of a K-step");
   constexpr int EB = EPI == EPI_GELU_FP8 ? NW * 32 * (WTN + 16) + WGN * BM * 4 : NW * 32 * (WTN * 4 + 16);
   constexpr int LDSB = STAGES * (SBUF + SSET) > EB ? STAGES * (SBUF + SSET) : EB;
-  __shared__ __attribute__((aligned(16))) char lds[LDSB];
+  // (integers: the factors of the tile's rows and columns, read once, behind the stages)
+  constexpr int FB = I8 ? ((BM + 2 * BN) * 4 + 255) / 256 * 256 : 0;
+  __shared__ __attribute__((aligned(16))) char lds[LDSB + FB];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WGN, wn = wave % WGN;
@@ -351,8 +380,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   // Scale DMA x < SA: 64 rows of A from 64 x on; SA: the weight blocks of the
   // tile's columns (those beyond it repeat SA's in places of their own). Wave w
   // issues w, w + NW, ...
-  u32x4 sdesc[SX];
-  uint32_t sofs[SX];
+  u32x4 sdesc[SX + 1];
+  uint32_t sofs[SX + 1];
 #pragma unroll
   for (int y = 0; y < SX; ++y) {
     const int x = wave + NW * y;
@@ -361,6 +390,25 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
                      : (uint32_t)min(lane, ((p.N - 1) >> 7) - (n0 >> 7)) * (uint32_t)p.ldsw;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  if constexpr (I8) {
+    // sa of the tile's rows, sw and bias of its columns: 64 a DMA instruction, ahead of the
+    // K tiles' (so the wait for the first of those covers them). Beyond M and N, and
+    // without a bias, descriptors end and zeros are read.
+    static_assert(BM % 32 == 0 && BN % 64 == 0, "whole DMA blocks of factors");
+    const float* src[3] = {reinterpret_cast<const float*>(p.sa) + m0, reinterpret_cast<const float*>(p.sw) + n0,
+                           p.bias + n0};
+#pragma unroll
+    for (int f = 0; f < 3; ++f) {
+      const int first = f == 0 ? 0 : f == 1 ? BM : BM + BN, blocks = f == 0 ? SA : BN / 64;
+      u32x4 d = descriptor(src[f]);
+      d[2] = f == 2 && !p.bias ? 0u : (uint32_t)min(f == 0 ? p.M - m0 : p.N - n0, f == 0 ? BM : BN) * 4u;
+      for (int x = wave; x < blocks; x += NW) {
+        const uint32_t at = (uint32_t)(64 * x + lane) * 4u, dst = lds0 + (uint32_t)(LDSB + first * 4 + x * 256);
+        if (BM >= 64 || f || lane < BM)
+          asm volatile("buffer_load_dword %0, %1, 0 offen lds" : : "v"(at), "s"(d), "{m0}"(dst) : "memory");
+      }
+    }
+  }
   // DMA instruction q of K tile t (t < KT)
   auto fetch1 = [&](int q, int t, int stage) {
     const uint32_t k = (uint32_t)t * KTB;
@@ -393,18 +441,18 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
       wad[ks][x] = lds0 + ABUF + (wn * WTN + r32) * KTB + ch;
       asm("" : "+v"(aad[ks][x]), "+v"(wad[ks][x]));
     }
-  f32x16 acc[TM][TN];                              // from the bias on
+  Acc<OPS> acc[TM][TN];                            // from the bias on
 #pragma unroll
   for (int j = 0; j < TN; ++j)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int col = n0 + wn * WTN + j * 32 + 8 * q + 4 * g;
       f32x4 b{0.0f, 0.0f, 0.0f, 0.0f};
-      if (p.bias && col < p.N) b = *reinterpret_cast<const f32x4*>(p.bias + col);
+      if (!I8 && p.bias && col < p.N) b = *reinterpret_cast<const f32x4*>(p.bias + col);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = b[e];
+        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = I8 ? 0 : b[e];
     }
   union Frag { i32x8 v; u32x4 h[2]; };
   Frag fa[TM], fw[2][TN];
@@ -422,11 +470,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   const uint32_t sad = lds0 + (uint32_t)(STAGES * SBUF + (wm * WTM + r32) * 4);
   const uint32_t swd = lds0 + (uint32_t)(STAGES * SBUF + (64 * SA + (((n0 & 127) + wn * WTN) >> 7)) * 4);
   auto read_scales = [&](int stage) {
+    if constexpr (I8) return;
 #pragma unroll
     for (int i = 0; i < TM; ++i) nsa[i] = *(lds_u32*)(uintptr_t)(sad + (uint32_t)(stage * SSET + i * 128));
     nsw = *(lds_u32*)(uintptr_t)(swd + (uint32_t)(stage * SSET));
   };
   auto take_scales = [&](int t) {                  // the byte of K tile t lowest
+    if constexpr (I8) return;
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = nsa[i] >> (8 * (t & 3));
     sw = nsw >> (8 * (t & 3));
@@ -447,10 +497,19 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
       }
       fence();
       return;
-    }
+    } else if constexpr (I8) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const i32x4 w = __builtin_bit_cast(i32x4, fw[set][j].h[x]), a = __builtin_bit_cast(i32x4, fa[i].h[x]);
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, a, acc[i][j], 0, 0, 0);
+      }
+      fence();
+      return;
+    } else {
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw[set][j].v, fa[i].v, acc[i][j], 0, 0, 0, (int)sw, 0,
                                                                 (int)sa[i]);
     fence();
+    }
   };
   if constexpr (STAGES == 1) {
     // One stage: the wait for a tile is hidden by the CU's other workgroups, and each
@@ -608,7 +667,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
   }
   wait_vm<0>();
   __syncthreads();                                 // no DMA in flight, every wave past its last fragment read
-  gemm8_epilogue<TM, TN, WTM, WTN, BM, BN, WGN, OCC, LDSB, EPI>(p, acc, lds, m0, n0, wm, wn, lane);
+  gemm8_epilogue<TM, TN, WTM, WTN, BM, BN, WGN, OCC, LDSB, EPI, OPS>(
+      p, acc, lds, m0, n0, wm, wn, lane, reinterpret_cast<const float*>(lds + LDSB));
 }
 
 // Column groups of the XCD tile partition (as the bf16 projections choose it).
@@ -629,12 +689,12 @@ inline int choose_xq(int M, int N, int K, int BM, int BN) {
   return best;
 }
 
-template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI, bool WIDE = false>
+template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI, int OPS = OPS_FP8>
 hipError_t launch_dma(const Gemm8Args& a0, hipStream_t s) {
   Gemm8Args a = a0;
   a.xq = choose_xq(a.M, a.N, a.K, BM, BN);
   const int64_t tiles = (int64_t)((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM);
-  launch((k_gemm8_dma<BM, BN, WGM, WGN, STAGES, OCC, EPI, DPI, WIDE>), dim3((uint32_t)tiles), dim3(64 * WGM * WGN), 0,
+  launch((k_gemm8_dma<BM, BN, WGM, WGN, STAGES, OCC, EPI, DPI, OPS>), dim3((uint32_t)tiles), dim3(64 * WGM * WGN), 0,
          s, a);
   return hipGetLastError();
 }
@@ -712,11 +772,11 @@ hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   if constexpr (EPI == EPI_RESID) {
     if (a.K > kResidWideK) {
       switch (choose_tiles(kTile8WideCost, a.M, a.N, a.K, EPI)) {
-        case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1, true>(a, s);
-        case 1: return launch_dma<128, 128, 2, 2, 1, 2, EPI, 4, true>(a, s);
-        case 2: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2, true>(a, s);
-        case 3: return launch_dma<64, 64, 2, 2, 4, 2, EPI, 4, true>(a, s);
-        case 4: return launch_dma<32, 64, 1, 2, 5, 1, EPI, 4, true>(a, s);
+        case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1, OPS_FP8_WIDE>(a, s);
+        case 1: return launch_dma<128, 128, 2, 2, 1, 2, EPI, 4, OPS_FP8_WIDE>(a, s);
+        case 2: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2, OPS_FP8_WIDE>(a, s);
+        case 3: return launch_dma<64, 64, 2, 2, 4, 2, EPI, 4, OPS_FP8_WIDE>(a, s);
+        case 4: return launch_dma<32, 64, 1, 2, 5, 1, EPI, 4, OPS_FP8_WIDE>(a, s);
       }
       return hipErrorInvalidValue;
     }
@@ -739,7 +799,37 @@ hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
+template <int EPI>
+hipError_t launch_epi_i8(const Gemm8Args& a, hipStream_t s) {
+  switch (choose_tiles(kTile8Cost, a.M, a.N, a.K, EPI)) {
+    case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1, OPS_I8>(a, s);
+    case 1: return launch_dma<192, 256, 2, 4, 2, 2, EPI, 1, OPS_I8>(a, s);
+    case 2: return launch_dma<128, 256, 2, 4, 3, 2, EPI, 1, OPS_I8>(a, s);
+    case 3: return launch_dma<128, 128, 2, 2, 1, 4, EPI, 4, OPS_I8>(a, s);
+    case 4: return launch_dma<64, 128, 2, 2, 3, 2, EPI, 2, OPS_I8>(a, s);
+    case 5: return launch_dma<32, 128, 1, 4, 3, 2, EPI, 4, OPS_I8>(a, s);
+    case 6: return launch_dma<64, 64, 2, 2, 4, 2, EPI, 4, OPS_I8>(a, s);
+    case 7: return launch_dma<32, 64, 1, 2, 5, 1, EPI, 4, OPS_I8>(a, s);
+    case 8: return launch_dma<128, 128, 2, 4, 4, 2, EPI, 1, OPS_I8>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
 }  // namespace
+
+hipError_t launch_gemm_i8(int epi, int M, int N, int K, const void* A, int64_t lda, const float* sa, const void* W,
+                          int64_t ldw, const float* sw, const float* bias, const float* gate, void* out, int64_t ldo,
+                          float* resid, int64_t ldr, hipStream_t s) {
+  if (M == 0) return hipSuccess;
+  Gemm8Args a{M, N, K, (const uint8_t*)A, lda, (const uint8_t*)sa, 0, (const uint8_t*)W, ldw, (const uint8_t*)sw, 0,
+              bias, gate, out, ldo, nullptr, 0, resid, ldr, 1};
+  switch (epi) {
+    case EPI_STORE: return launch_epi_i8<EPI_STORE>(a, s);
+    case EPI_GELU: return launch_epi_i8<EPI_GELU>(a, s);
+    case EPI_RESID: return launch_epi_i8<EPI_RESID>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
 
 hipError_t launch_gemm_fp8(int epi, int M, int N, int K, const void* A, int64_t lda, const void* sa, int64_t ldsa,
                            const void* W, int64_t ldw, const void* sw, int64_t ldsw, const float* bias,

@@ -1,4 +1,5 @@
-// Host entry points of the 8-bit operators' kernels (k_gemm8.hip, k_fp8rows.hip).
+// Host entry points of the 8-bit operators' kernels (k_gemm8.hip, k_fp8rows.hip,
+// k_i8rows.hip).
 #pragma once
 
 #include "kernels.h"
@@ -17,6 +18,19 @@ hipError_t launch_gemm_fp8(int epi, int M, int N, int K, const void* A, int64_t 
                            const void* W, int64_t ldw, const void* sw, int64_t ldsw, const float* bias,
                            const float* gate, void* out, int64_t ldo, void* so, int64_t ldso, float* resid,
                            int64_t ldr, hipStream_t s);
+
+// launch_gemm on 8-bit integers: sa float32 [M], sw [N]; EPI_STORE, EPI_GELU (out in
+// bf16) and EPI_RESID. Bias may be null. N, K and the operands' row strides multiples
+// of 16, K at most kI8MaxK.
+constexpr int kI8MaxK = 133120;                    // K * 127^2 below 2^31
+hipError_t launch_gemm_i8(int epi, int M, int N, int K, const void* A, int64_t lda, const float* sa, const void* W,
+                          int64_t ldw, const float* sw, const float* bias, const float* gate, void* out, int64_t ldo,
+                          float* resid, int64_t ldr, hipStream_t s);
+
+// 8-bit integers and float32 scales of the rows of x [rows][K] (f32 or bf16); K a
+// multiple of 8.
+hipError_t launch_quant_i8(int dt, int rows, int K, const void* x, int64_t ldx, void* q, int64_t ldq, float* scale,
+                           hipStream_t s);
 
 // e4m3 values and E8M0 scales of x [rows][K] (f32 or bf16) per block_rows (1 or
 // 128) x 128; K a multiple of 8.

@@ -13,7 +13,7 @@ import ctypes
 import functools
 import os
 import re
-from typing import Dict, Optional, Sequence
+from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -22,7 +22,8 @@ LIB_PATH = os.path.join(HERE, "lib", "libf3c.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "f3c.h")
 
 F3C_OK, F3C_EINVAL, F3C_ENOMEM, F3C_EHIP, F3C_ESTATE = 0, -1, -2, -3, -4
-F3C_F32, F3C_BF16, F3C_FP8 = 0, 1, 2
+F3C_F32, F3C_BF16, F3C_FP8, F3C_I8 = 0, 1, 2, 3
+F3C_PAGE_TOKENS = 64
 F3C_NORM_NONE, F3C_NORM_LAYER, F3C_NORM_RMS = 0, 1, 2
 F3C_STATE_GUIDED = 1
 PROF_CLASSES = ["select", "embed", "mod", "ln", "gemm_qkv", "attn_self", "gemm_o", "gemm_q", "attn_cross",
@@ -49,6 +50,11 @@ class ModelCfg(ctypes.Structure):
 class ResidNormCfg(ctypes.Structure):
     _fields_ = [("dtype", c_int), ("out_dtype", c_int), ("post", c_int), ("pre", c_int), ("eps", c_f),
                 ("resid_scale", c_f)]
+
+
+class Cache8Args(ctypes.Structure):
+    _fields_ = [(n, c_int) for n in ("kv_heads", "head_dim", "n_pages", "max_pages")] + [
+        (n, c_p) for n in ("k", "v", "k_scale", "v_scale", "table")]
 
 
 _SIGS = {
@@ -100,6 +106,15 @@ _SIGS = {
                                 c_p, c_int, c_p, c_int, c_p, c_int, c_p]),
     "f3c_op_resid_norm": (c_int, [ctypes.POINTER(ResidNormCfg), c_int, c_int, P_i32, c_p, c_int, c_p, c_p, c_p, c_int,
                                   c_p, c_p, c_p, c_int, c_p, c_int, c_p, c_int, c_p]),
+    "f3c_op_quant_i8": (c_int, [c_int, c_int, c_int, c_p, c_int, c_p, c_int, c_p, c_p]),
+    "f3c_op_gemm_i8": (c_int, [c_int, c_int, c_int, c_int, c_p, c_int, c_p, c_p, c_int, c_p, c_p, c_p, c_p, c_int, c_p,
+                               c_int, c_p]),
+    "f3c_op_cache8_append": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, P_i32, P_i32, c_p, c_int, c_p, c_int,
+                                     c_p]),
+    "f3c_op_cache8_attention_bytes": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, P_i32, P_i32, c_int,
+                                              ctypes.POINTER(c_sz)]),
+    "f3c_op_cache8_attention": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, P_i32, P_i32, c_p, c_int, c_p, c_int,
+                                        c_int, c_int, c_p, c_sz, c_p]),
     "f3c_op_modulation": (c_int, [c_p, c_d, c_p, c_p, c_p]),
     "f3c_op_embed": (c_int, [c_p, c_int, c_p, c_p, P_i32, c_p, c_p]),
     "f3c_op_final": (c_int, [c_p, c_int, c_p, c_p, c_p]),
@@ -546,7 +561,7 @@ def _dtypes():
     if _types is None:
         import torch
         fp8, byte = torch.float8_e4m3fn, torch.uint8
-        _types = {F3C_F32: (torch.float32,), F3C_BF16: (torch.bfloat16,), F3C_FP8: (fp8, byte),
+        _types = {F3C_F32: (torch.float32,), F3C_BF16: (torch.bfloat16,), F3C_FP8: (fp8, byte), F3C_I8: (torch.int8,),
                   "scale": (torch.float8_e8m0fnu, byte), "torch": torch}
     return _types
 
@@ -650,6 +665,131 @@ def op_gemm_fp8(epilogue: int, A, A_scale, W, W_scale, bias=None, out=None, out_
         *(none if out is None else _rows("out", out, fp8 if epilogue == 3 else T[F3C_BF16], M, N, dev)),
         *(none if out_scale is None else _scale_rows("out_scale", out_scale, T["scale"], M, N, dev)),
         *(none if resid is None else _rows("resid", resid, f32, M, N, dev)), _stream_on(stream, dev, T["torch"])))
+
+
+def op_quant_i8(dtype: int, x, q, scale, stream=None):
+    """x [R][K] -> q (int8 [R][K]) and scale (float32 [R]), one scale a row: tokens of activations, output channels of
+    weights."""
+    T = _dtypes()
+    if dtype not in (F3C_F32, F3C_BF16) or x.dim() != 2:
+        raise ValueError("rows of dtype F3C_F32 or F3C_BF16 expected")
+    R, K = x.shape
+    dev = _device(x, T["torch"])
+    check((_lib or lib()).f3c_op_quant_i8(
+        dtype, R, K, *_rows("x", x, T[dtype], R, K, dev), *_rows("q", q, T[F3C_I8], R, K, dev),
+        _vector("scale", scale, T[F3C_F32], R, dev), _stream_on(stream, dev, T["torch"])))
+
+
+def op_gemm_i8(epilogue: int, A, A_scale, W, W_scale, bias=None, out=None, resid=None, gate=None, stream=None):
+    """op_gemm on 8-bit integers (op_quant_i8's): A int8 [M][K], W int8 [N][K], a float32 scale for each of their rows."""
+    T = _dtypes()
+    if epilogue not in (0, 1, 2) or A.dim() != 2 or W.dim() != 2:
+        raise ValueError("epilogue 0..2 and rows of A and W expected")
+    if (out is None) != (epilogue == 2) or (resid is None) != (epilogue != 2):
+        raise ValueError("epilogues 0 and 1 write out, 2 updates resid")
+    if A_scale is None or W_scale is None:
+        raise ValueError("a scale for each row of A and W expected")
+    M, K = A.shape
+    N = W.shape[0]
+    dev = _device(A, T["torch"])
+    none, f32, i8 = (None, 0), T[F3C_F32], T[F3C_I8]
+    check((_lib or lib()).f3c_op_gemm_i8(
+        epilogue, M, N, K, *_rows("A", A, i8, M, K, dev), _vector("A_scale", A_scale, f32, M, dev),
+        *_rows("W", W, i8, N, K, dev), _vector("W_scale", W_scale, f32, N, dev), _vector("bias", bias, f32, N, dev),
+        _vector("gate", gate, f32, N, dev), *(none if out is None else _rows("out", out, T[F3C_BF16], M, N, dev)),
+        *(none if resid is None else _rows("resid", resid, f32, M, N, dev)), _stream_on(stream, dev, T["torch"])))
+
+
+# ------------------------------------------------------- keys and values in 8 bits
+
+class Cache8(NamedTuple):
+    """A pool of pages of 64 tokens and the pages of each sample (f3c_cache8): k e4m3 [pages][heads][64][head_dim],
+    v [pages][heads][head_dim][64], k_scale and v_scale E8M0 bytes [pages][heads], table int32 [samples][pages of one].
+    Contiguous tensors on one GPU."""
+    k: object
+    v: object
+    k_scale: object
+    v_scale: object
+    table: object
+
+    @classmethod
+    def empty(cls, n_pages: int, kv_heads: int, head_dim: int, table, device="cuda"):
+        """A pool without tokens (no page is read before it has been written)."""
+        import torch
+        e = lambda *s: torch.empty(*s, dtype=torch.uint8, device=device)  # noqa: E731
+        return cls(e(n_pages, kv_heads, F3C_PAGE_TOKENS, head_dim), e(n_pages, kv_heads, head_dim, F3C_PAGE_TOKENS),
+                   e(n_pages, kv_heads), e(n_pages, kv_heads), table)
+
+
+def _cache8(cache, batch: int, dev: int, T):
+    """The cache as the C call's argument, its key heads and their width."""
+    k, v, ks, vs, table = cache
+    fp8 = T[F3C_FP8]
+    pages, heads, page, hd = k.shape if k.dim() == 4 else (0, 0, 0, 0)
+    if (page != F3C_PAGE_TOKENS or k.dtype not in fp8 or v.dtype not in fp8 or v.shape != (pages, heads, hd, page)
+            or ks.shape != (pages, heads) or vs.shape != (pages, heads) or ks.dtype not in T["scale"]
+            or vs.dtype not in T["scale"] or table.dim() != 2 or table.shape[0] < batch
+            or table.dtype != T["torch"].int32):
+        raise ValueError("cache: k e4m3 [pages][heads][64][head_dim], v [pages][heads][head_dim][64], scale bytes "
+                         "[pages][heads], table int32 [samples][pages of one] expected")
+    for t in cache:
+        if t.get_device() != dev or not t.is_contiguous():
+            raise ValueError("cache: contiguous tensors on the current GPU expected")
+    return Cache8Args(heads, hd, pages, table.shape[1], k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(),
+                      table.data_ptr()), heads, hd
+
+
+def _samples(off, lens, rows: int):
+    """(row offsets, samples, tokens held) as C values."""
+    offsets, B, lowest, highest = _offsets(tuple(map(int, off)))
+    if B < 1 or lowest < 0 or highest > rows or len(lens) != B:
+        raise ValueError("off: B + 1 row offsets within the rows, lens: B token counts expected")
+    return offsets, B, _i32(lens)
+
+
+def op_cache8_append(dtype: int, cache, lens: Sequence[int], off: Sequence[int], k, v, stream=None):
+    """Rows off[b]..off[b+1] of k and v [R][heads * head_dim] become tokens lens[b].. of sample b (cache: a Cache8, or its
+    five tensors)."""
+    T = _dtypes()
+    if dtype not in (F3C_F32, F3C_BF16) or k.dim() != 2:
+        raise ValueError("rows of dtype F3C_F32 or F3C_BF16 expected")
+    R = k.shape[0]
+    dev = _device(k, T["torch"])
+    offsets, B, held = _samples(off, lens, R)
+    args, heads, hd = _cache8(cache, B, dev, T)
+    check((_lib or lib()).f3c_op_cache8_append(
+        ctypes.byref(args), dtype, B, held, offsets, *_rows("k", k, T[dtype], R, heads * hd, dev),
+        *_rows("v", v, T[dtype], R, heads * hd, dev), _stream_on(stream, dev, T["torch"])))
+
+
+def op_cache8_attention(cache, heads: int, q_off: Sequence[int], lens: Sequence[int], q, o, causal: bool = False,
+                        q_prescaled: bool = False, workspace=None, stream=None):
+    """Attention of bf16 queries q [R][heads * head_dim] over the lens[b] tokens that the cache holds of each sample,
+    into o. workspace: a device tensor that the call may use, as large as it is (allocated here if None)."""
+    T = _dtypes()
+    torch = T["torch"]
+    if q.dim() != 2:
+        raise ValueError("rows of queries expected")
+    R = q.shape[0]
+    dev = _device(q, torch)
+    offsets, B, held = _samples(q_off, lens, R)
+    args, _, hd = _cache8(cache, B, dev, T)
+    L = _lib or lib()
+    cache_p, on = ctypes.byref(args), _stream_on(stream, dev, torch)
+    if workspace is None:
+        need = c_sz()
+        check(L.f3c_op_cache8_attention_bytes(cache_p, heads, B, offsets, held, int(causal), ctypes.byref(need)))
+        if need.value:
+            # (memory of the stream that the call runs on: it is free again once that stream is past the call)
+            with torch.cuda.stream(None if stream is None else torch.cuda.ExternalStream(on)):
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the current GPU expected")
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    check(L.f3c_op_cache8_attention(cache_p, heads, B, offsets, held,
+                                    *_rows("q", q, T[F3C_BF16], R, heads * hd, dev),
+                                    *_rows("o", o, T[F3C_BF16], R, heads * hd, dev), int(causal), int(q_prescaled),
+                                    _ptr(workspace), size, on))
 
 
 @functools.lru_cache(maxsize=256)
