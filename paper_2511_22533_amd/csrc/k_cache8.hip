@@ -1,5 +1,6 @@
 // The cache of 8-bit keys and values (cache8.h): appending to it, and attention over it.
 #include <algorithm>
+#include <utility>
 
 #include "cache8.h"
 #include "fp8.h"
@@ -352,15 +353,411 @@ __global__ __launch_bounds__(64 * NW) void k_cache8_attn(Attn8Args p) {
   }
 }
 
-// The splits' results, joined in their order: a thread has four columns of a row.
-template <int HD>
-__global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p) {
+// What lane ^ 32 holds beside v: the larger of the two, or their sum, in both.
+__device__ __forceinline__ float half_max(float v) {
+  float w = v;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(v), "+v"(w));
+  return fmaxf(v, w);
+}
+__device__ __forceinline__ float half_sum(float v) {
+  float w = v;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(v), "+v"(w));
+  return v + w;
+}
+
+// f(std::integral_constant<int, I>) for I = 0 .. N - 1, unrolled.
+template <typename F, int... I>
+__device__ __forceinline__ void static_for_seq(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F f) {
+  static_for_seq(f, std::make_integer_sequence<int, N>{});
+}
+
+// The largest of a tile's 16 scores: dependent v_max3 in one block (fmaxf would quiet each
+// operand first). NaN is passed over; its probability is NaN all the same.
+__device__ __forceinline__ float max16(const f32x16& v) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3\n\t"
+      "v_max3_f32 %0, %0, %4, %5\n\t"
+      "v_max3_f32 %0, %0, %6, %7\n\t"
+      "v_max3_f32 %0, %0, %8, %9\n\t"
+      "v_max3_f32 %0, %0, %10, %11\n\t"
+      "v_max3_f32 %0, %0, %12, %13\n\t"
+      "v_max3_f32 %0, %0, %14, %15\n\t"
+      "v_max_f32 %0, %0, %16"
+      : "=&v"(r)
+      : "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]), "v"(v[8]), "v"(v[9]),
+        "v"(v[10]), "v"(v[11]), "v"(v[12]), "v"(v[13]), "v"(v[14]), "v"(v[15]));
+  return r;
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Many rows: NW waves of 32 rows each share a page, which goes to LDS by DMA as it
+// is, STAGES deep, its 16-byte chunks swizzled by row for conflict-free fragment reads;
+// fragments are widened as they are read. Scores on 32 x 32 instructions, S^T = K Q^T.
+//
+// Pages that all rows of a wave see go in half steps of 32 keys: the matrix cores take the
+// scores of the next 32 keys and the product with V of the 32 before while the vector
+// unit takes the probabilities of these, instruction by instruction (a barrier to the
+// compiler's scheduler behind each group; left alone it gathers the products and then the
+// vector work, and both waves of a SIMD wait for the same unit). Pages at a row's limit, at
+// most a few and the last, go one step after the other, with masks.
+template <int HD, int NW, bool SPLIT>
+__global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn8Args p) {
+  constexpr int ROWS = 32 * NW, TILE = kPage * HD, STAGES = 5;
+  constexpr int NS = HD / 32, NV = HD / 32;        // pairs of K slices of 16 columns; output tiles of 32
+  constexpr int CPR = HD / 16;                     // 16-byte chunks of a row of K
+  constexpr int DMA = TILE / 1024;                 // DMA instructions per tile
+  constexpr int DQ = 2 * DMA / NW;                 // of both tiles, per wave
+  static_assert(2 * DMA % NW == 0, "whole DMA blocks per wave");
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * TILE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = lane >> 5, r32 = lane & 31;
   const int n_tiles = p.tiles.off[p.tiles.B], kvh = p.c.kv_heads;
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, slot = x / (HD / 4), all = (int64_t)n_tiles * kvh * 16;
+  int item = xcd_logical_id(blockIdx.x, n_tiles * kvh * p.splits);
+  const int split = item % p.splits;
+  item /= p.splits;
+  const int head = item / n_tiles, tile = n_tiles - 1 - item % n_tiles;      // (causal: the longest first)
+  const int b = find_segment_wave(p.tiles.off, p.tiles.B, tile);
+  const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
+  const int row_t = (tile - p.tiles.off[b]) * ROWS, row_w = row_t + wave * 32;
+  const int row = row_w + r32, tok = row / p.group, qcol = (head * p.group + row - tok * p.group) * HD;
+  const int lim = tok >= nq ? 0 : p.causal ? max(min(n, n - nq + tok + 1), 0) : n;
+  // the wave's lowest limit, its highest, the workgroup's highest
+  const int lim_lo = p.causal ? n - nq + row_w / p.group + 1 : n;
+  const int lim_w = row_w >= nq * p.group ? 0
+                    : p.causal ? max(n - nq + min((row_w + 31) / p.group, nq - 1) + 1, 0) : n;
+  const int lim_hi = p.causal ? max(n - nq + min((row_t + ROWS - 1) / p.group, nq - 1) + 1, 0) : n;
+  const int pages = (lim_hi + kPage - 1) / kPage;
+  const int begin = (int)((int64_t)split * pages / p.splits), end = (int)((int64_t)(split + 1) * pages / p.splits);
+
+  // Columns of a lane's fragment 2 i + h: 32 i + 16 g + 8 h on, as a chunk of K holds them.
+  bf16x8 qf[2 * NS];
+#pragma unroll
+  for (int s = 0; s < 2 * NS; ++s) {
+    u32x4 raw{0, 0, 0, 0};
+    if (tok < nq)
+      raw = *reinterpret_cast<const u32x4*>(p.q + (q0 + tok) * p.ldq + qcol + 32 * (s / 2) + 16 * g + 8 * (s % 2));
+    qf[s] = __builtin_bit_cast(bf16x8, raw);
+  }
+  // o: outputs; m: what probabilities are relative to (the largest score, base 2, or up to 2^8
+  // below it), above: the score from which on it moves; l: sums of a lane's own keys.
+  f32x16 o[NV];
+  float m = -INFINITY, above = -INFINITY;
+  f32x4 l{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int t = 0; t < NV; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+  // K: rows of CPR chunks, physical chunk = chunk ^ (row / (16 / CPR)) % CPR, so that 16
+  // lanes reading a chunk of 16 rows meet 16 different places of 256 bytes; V: rows of 4.
+  auto kswz = [](int row) { return row / (16 / CPR) & (CPR - 1); };
+  auto vswz = [](int row) { return row >> 2 & 3; };
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  // A lane's place within the 1 KiB that a DMA instruction reads (the same for all of a
+  // wave's: blocks are NW apart, and only their parity enters, of 128 columns alone).
+  static_assert(NW % 2 == 0, "a wave's blocks are all even or all odd");
+  const uint32_t kdma = (uint32_t)(lane / CPR * HD + ((lane % CPR ^ kswz(64 / CPR * wave + lane / CPR)) << 4));
+  const uint32_t vdma = (uint32_t)(lane / 4 * 64 + ((lane % 4 ^ vswz(lane / 4)) << 4));
+  // Fragment reads: rows r32 (and 32 further) of the tiles, chunks 2 x + g.
+  uint32_t kof[NS], vof[2];
+#pragma unroll
+  for (int x = 0; x < NS; ++x) kof[x] = lds0 + (uint32_t)(r32 * HD + ((2 * x + g ^ kswz(r32)) << 4));
+#pragma unroll
+  for (int x = 0; x < 2; ++x) vof[x] = lds0 + (uint32_t)(TILE + r32 * 64 + ((2 * x + g ^ vswz(r32)) << 4));
+  typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+  typedef __attribute__((address_space(3))) const u32x2 lds_u32x2;
+  auto read_k = [&](uint32_t at, int h, int x) { return *(lds_u32x4*)(uintptr_t)(kof[x] + at + (uint32_t)(h * 32 * HD)); };
+  auto read_v = [&](uint32_t at, int h, int t, int x) {               // words of tokens 32 h on
+    return *(lds_u32x2*)(uintptr_t)(vof[x] + at + (uint32_t)(t * 32 * 64 + 8 * h));
+  };
+  auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+  const f32x16 zero = {};
+
+  // The pages from `base` on, one a lane: its number (or none), its scales.
+  int pg = -1, base = 0;
+  float pks = 0.0f, pvs = 0.0f;
+  auto look = [&](int at) {
+    base = at;
+    pg = -1;
+    if (at + lane < end) pg = p.c.table[(int64_t)b * p.c.max_pages + at + lane];
+    if ((uint32_t)pg >= (uint32_t)p.c.n_pages) pg = -1;
+    const int64_t x = (int64_t)(pg < 0 ? 0 : pg) * kvh + head;
+    pks = fp8_scale(p.c.ks[x]);
+    pvs = fp8_scale(p.c.vs[x]);
+  };
+  auto lane_f = [](float v, int i) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
+  };
+  auto fetch = [&](int i, int stage) {             // page i (of those looked up); no page: the pool's first, unused
+    const int page = max(__builtin_amdgcn_readlane(pg, i - base), 0);
+    const int64_t at = ((int64_t)page * kvh + head) * TILE;
+#pragma unroll
+    for (int q = 0; q < DQ; ++q) {
+      const int blk = wave + NW * q, of = blk < DMA ? blk : blk - DMA;
+      const uint8_t* from = (blk < DMA ? p.c.k : p.c.v) + at + of * 1024;
+      const uint32_t to = lds0 + (uint32_t)(stage * 2 * TILE + blk * 1024);
+      asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(blk < DMA ? kdma : vdma), "s"(from), "{m0}"(to) : "memory");
+    }
+  };
+  // The reference moves to `to`: what was summed up is scaled.
+  auto rescale = [&](float to) __attribute__((always_inline)) {
+    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    above = (to + 8.0f) / p.scale;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) l[e] *= f;
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] *= f;
+  };
+  auto row_sum = [](const bf16x8& f, f32x4 acc) {  // of a lane's own values: 4 x 4 blocks, ones on the left
+    const s16x4 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
+    union { bf16x8 b; s16x4 h[2]; } u{f};
+    acc = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(one, u.h[0], acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(one, u.h[1], acc, 0, 0, 0);
+  };
+
+  // A page with masks, one step after the other.
+  auto masked_page = [&](int i, uint32_t at, float ks, float vs) __attribute__((always_inline)) {
+    // (tokens counted from the lane's first; opaque, or the compiler keeps 64 sums over all pages)
+    int there = n - i * kPage - 4 * g, seen = lim - i * kPage - 4 * g;
+    asm("" : "+v"(there), "+v"(seen));
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+      f32x16 s;
+#pragma unroll
+      for (int x = 0; x < NS; ++x) {
+        const u32x4 w = read_k(at, h, x);
+        const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * x], x ? s : zero, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[2 * x + 1], s, 0, 0, 0);
+        fence();
+      }
+      bf16x8 pf[2];
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (8 * (e / 4) + e % 4 >= seen) s[e] = -INFINITY;
+      const float mx = half_max(max16(s));
+      if (__any(mx > above)) rescale(fmaxf(m, mx * p.scale));
+      const float ref = m == -INFINITY ? 0.0f : -m;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        pf[e / 8][e % 8] = (bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale, ref));
+#pragma unroll
+      for (int u = 0; u < 2; ++u) l = row_sum(pf[u], l);
+      fence();
+#pragma unroll
+      for (int t = 0; t < NV; ++t) {
+        u32x2 v[2];
+        // (as for 16 rows: what was never written counts as 0, and NaN where it is seen)
+        uint32_t odd = 0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          v[x] = read_v(at, h, t, x);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int left = there - 16 * u - 8 * x;
+            v[x][u] &= left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+            odd |= nan_bytes(v[x][u]);
+          }
+        }
+        if (__any(odd)) {
+          f32x16 count = zero;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            bf16x8 sees;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              sees[e] = (bf16)(16 * u + 8 * (e / 4) + e % 4 < seen ? 1.0f : 0.0f);
+            count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                widen8(nan_bytes(v[0][u]) & 0x38383838u, nan_bytes(v[1][u]) & 0x38383838u, 1.0f), sees, count, 0, 0, 0);
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (count[e] > 0.0f) o[t][e] = __builtin_nanf("");
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) v[x][u] &= ~nan_bytes(v[x][u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 vf = widen8(v[0][u], v[1][u], vs);
+          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[u], o[t], 0, 0, 0);
+        }
+        fence();
+      }
+      there -= 32;
+      seen -= 32;
+    }
+  };
+
+  // A half step: scores `next` of half KH of the page at `kat`, probabilities pc of `cur`, the
+  // product of pp with half VH of the page at `vat`.
+  u32x4 kr[2];                                     // raw fragments of K (a pair of slices each)
+  u32x2 vr[2][2];                                  // and of V (an output tile each)
+  auto product_v = [&](uint32_t vat, int h, float vs, bf16x8 (&pp)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < NV; ++t) {
+      const u32x2 a = read_v(vat, h, t, 0), c = read_v(vat, h, t, 1);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 vf = widen8(a[u], c[u], vs);
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pp[u], o[t], 0, 0, 0);
+      }
+      fence();
+    }
+    pp[0] = pp[1] = bf16x8{};
+  };
+  auto half_step = [&](auto hc, uint32_t kat, float ks, uint32_t vat, float vs, const f32x16& cur,
+                       f32x16& next, bf16x8 (&pp)[2], bf16x8 (&pc)[2]) __attribute__((always_inline)) {
+    constexpr int KH = decltype(hc)::value, VH = KH;                   // (i, 0): K of (i, 1), V of (i - 1, 1); ...
+    const float mx = half_max(max16(cur));
+    if (__any(mx > above)) {                       // rare
+      product_v(vat, VH, vs, pp);
+      rescale(fmaxf(m, mx * p.scale));
+    }
+    constexpr int G = 4 * NS, N = 16;              // groups of a product, K and V in turn; probabilities
+    float ex[N];
+    bf16x8 kf, vf;
+    kr[0] = read_k(kat, KH, 0);
+    vr[0][0] = read_v(vat, VH, 0, 0);
+    vr[0][1] = read_v(vat, VH, 0, 1);
+    static_for<G>([&](auto nc) {
+      constexpr int x = decltype(nc)::value, a = x / 2;
+      if constexpr (x % 4 == 0 && x + 4 < G) {
+        kr[(a / 2 + 1) % 2] = read_k(kat, KH, a / 2 + 1);
+        vr[(a / 2 + 1) % 2][0] = read_v(vat, VH, a / 2 + 1, 0);
+        vr[(a / 2 + 1) % 2][1] = read_v(vat, VH, a / 2 + 1, 1);
+      }
+      if constexpr (x % 2 == 0) {
+        kf = widen8(kr[a / 2 % 2][2 * (a % 2)], kr[a / 2 % 2][2 * (a % 2) + 1], ks);
+        next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[a], a ? next : zero, 0, 0, 0);
+      } else {
+        vf = widen8(vr[a / 2 % 2][0][a % 2], vr[a / 2 % 2][1][a % 2], vs);
+        o[a / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pp[a % 2], o[a / 2], 0, 0, 0);
+      }
+      constexpr int E0 = x * N / G, E1 = (x + 1) * N / G;
+      static_for<E1 - E0>([&](auto k) {
+        constexpr int i = E0 + decltype(k)::value;
+        ex[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[i], p.scale, -m));
+        if constexpr (i % 2) {
+          pc[i / 8][i % 8 - 1] = (bf16)ex[i - 1];
+          pc[i / 8][i % 8] = (bf16)ex[i];
+        }
+        if constexpr (i % 8 == 7) l = row_sum(pc[i / 8], l);
+      });
+      fence();
+    });
+  };
+
+  const std::integral_constant<int, 0> h0{};
+  const std::integral_constant<int, 1> h1{};
+  for (int first = begin; first < end; first += 64) {
+    const int last = min(first + 64, end);
+    __syncthreads();                               // every wave past its reads of the last stages
+    look(first);
+    wait_vm<0>();
+#pragma unroll
+    for (int i = 0; i < STAGES - 2; ++i) fetch(min(first + i, last - 1), i);
+    int stage = 0;                                 // of page i
+    auto sync = [&](int i) {                       // page i + 1 has landed (and i), the stage of i - 2 is free
+      wait_vm<(STAGES - 4) * DQ>();
+      __builtin_amdgcn_s_barrier();
+      fence();
+      fetch(min(i + STAGES - 2, last - 1), stage >= 2 ? stage - 2 : stage + STAGES - 2);
+    };
+    auto page_of = [&](int i) { return __builtin_amdgcn_readlane(pg, i - base); };
+    auto full = [&](int i) { return page_of(i) >= 0 && (i + 1) * kPage <= lim_lo; };
+    auto advance = [&] {
+      const uint32_t at = (uint32_t)(stage * 2 * TILE);
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
+      return at;
+    };
+    int i = first;
+    while (i < last) {
+      if (!full(i)) {
+        sync(i);
+        const uint32_t at = advance();
+        if (page_of(i) >= 0 && i * kPage < lim_w) masked_page(i, at, lane_f(pks, i - base), lane_f(pvs, i - base));
+        ++i;
+        continue;
+      }
+      // A run of whole pages. In front of its first half step the probabilities before are
+      // zeros, times V of its first page, which every row sees.
+      f32x16 s0, s1;
+      bf16x8 p0[2], p1[2];
+      sync(i);
+      uint32_t at = advance(), at_before = at;
+      float ks = lane_f(pks, i - base), vs = lane_f(pvs, i - base), vs_before = vs;
+      p1[0] = p1[1] = bf16x8{};
+#pragma unroll
+      for (int x = 0; x < NS; ++x) {
+        const u32x4 w = read_k(at, 0, x);
+        const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
+        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * x], x ? s0 : zero, 0, 0, 0);
+        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[2 * x + 1], s0, 0, 0, 0);
+        fence();
+      }
+      for (;;) {
+        const int ahead = min(i + 1, last - 1) - base;
+        const float ks_next = lane_f(pks, ahead), vs_next = lane_f(pvs, ahead);
+        half_step(h1, at, ks, at_before, vs_before, s0, s1, p1, p0);
+        half_step(h0, (uint32_t)(stage * 2 * TILE), ks_next, at, vs, s1, s0, p0, p1);
+        at_before = at, vs_before = vs;
+        ++i;
+        if (i >= last || !full(i)) break;
+        sync(i);
+        at = advance();
+        ks = ks_next, vs = vs_next;
+      }
+      product_v(at_before, 1, vs_before, p1);
+    }
+  }
+  wait_vm<0>();                                    // no DMA into LDS that another workgroup may get
+  const float sum = half_sum(l[0]);
+  if constexpr (SPLIT) {
+    const int64_t slot = (((int64_t)split * n_tiles + tile) * kvh + head) * ROWS + wave * 32 + r32;
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4*>(p.part_o + slot * HD + 32 * t + 2 * e + 4 * g) =
+            f32x4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]};
+    if (g == 0) {
+      p.part_ml[2 * slot] = m;
+      p.part_ml[2 * slot + 1] = sum;
+    }
+  } else if (tok < nq) {
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    bf16* out = p.o + (q0 + tok) * p.ldo + qcol;
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        bf16x4 w;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) w[x] = (bf16)(o[t][e + x] * inv);
+        *reinterpret_cast<bf16x4*>(out + 32 * t + 2 * e + 4 * g) = w;
+      }
+  }
+}
+
+// The splits' results, joined in their order: a thread has four columns of a row (ROWS a
+// tile).
+template <int HD>
+__global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p, int tile_rows) {
+  const int n_tiles = p.tiles.off[p.tiles.B], kvh = p.c.kv_heads;
+  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, slot = x / (HD / 4), all = (int64_t)n_tiles * kvh * tile_rows;
   if (slot >= all) return;
-  const int d = (int)(x % (HD / 4)) * 4, r = (int)(slot % 16), head = (int)(slot / 16 % kvh);
-  const int tile = (int)(slot / 16 / kvh), b = find_segment(p.tiles.off, p.tiles.B, tile);
-  const int row = (tile - p.tiles.off[b]) * 16 + r, t = row / p.group, q0 = p.rows.off[b];
+  const int d = (int)(x % (HD / 4)) * 4, r = (int)(slot % tile_rows), head = (int)(slot / tile_rows % kvh);
+  const int tile = (int)(slot / tile_rows / kvh), b = find_segment(p.tiles.off, p.tiles.B, tile);
+  const int row = (tile - p.tiles.off[b]) * tile_rows + r, t = row / p.group, q0 = p.rows.off[b];
   if (t >= p.rows.off[b + 1] - q0) return;
   float top = -INFINITY;
   for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[2 * (s * all + slot)]);
@@ -383,9 +780,9 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p) {
 
 struct Plan {
   Segs tiles;
-  int splits;
+  int rows, splits;                                // rows: of a tile
   size_t bytes(const Cache8& c) const {
-    return splits < 2 ? 0 : (size_t)splits * tiles.off[tiles.B] * c.kv_heads * 16 * (c.hd + 2) * 4;
+    return splits < 2 ? 0 : (size_t)splits * tiles.off[tiles.B] * c.kv_heads * rows * (c.hd + 2) * 4;
   }
 };
 
@@ -394,29 +791,36 @@ constexpr int kWaves = 4;
 Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len) {
   Plan r{};
   const int group = heads / c.kv_heads;
+  int64_t most = 0;
+  for (int b = 0; b < rows.B; ++b) most = std::max(most, (int64_t)(rows.off[b + 1] - rows.off[b]) * group);
+  r.rows = most <= 16 ? 16 : 128;
   r.tiles.B = rows.B;
   int pages = 0;
   for (int b = 0; b < rows.B; ++b) {
     const int64_t n = (int64_t)(rows.off[b + 1] - rows.off[b]) * group;
-    r.tiles.off[b + 1] = r.tiles.off[b] + (int)((n + 15) / 16);
+    r.tiles.off[b + 1] = r.tiles.off[b] + (int)((n + r.rows - 1) / r.rows);
     if (n) pages = std::max(pages, (len.n[b] + kPage - 1) / kPage);
   }
   const int64_t items = (int64_t)r.tiles.off[rows.B] * c.kv_heads;
   r.splits = 1;
-  if (items) r.splits = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / items, pages / (2 * kWaves)));
+  if (items) r.splits = (int)std::max<int64_t>(1, std::min<int64_t>((r.rows == 16 ? 1024 : 512) / items, pages / 8));
   return r;
 }
 
 template <int HD>
-hipError_t launch_attn8(const Attn8Args& a, hipStream_t s) {
+hipError_t launch_attn8(const Attn8Args& a, int rows, hipStream_t s) {
   const int64_t items = (int64_t)a.tiles.off[a.tiles.B] * a.c.kv_heads;
   if (!items) return hipSuccess;
-  if (a.splits < 2) {
-    launch((k_cache8_attn<HD, kWaves, false>), dim3((uint32_t)items), dim3(64 * kWaves), 0, s, a);
-    return hipGetLastError();
+  const dim3 grid((uint32_t)(items * a.splits));
+  if (rows == 16) {
+    if (a.splits < 2) launch((k_cache8_attn<HD, kWaves, false>), grid, dim3(64 * kWaves), 0, s, a);
+    else launch((k_cache8_attn<HD, kWaves, true>), grid, dim3(64 * kWaves), 0, s, a);
+  } else {
+    if (a.splits < 2) launch((k_cache8_rows<HD, 4, false>), grid, dim3(256), 0, s, a);
+    else launch((k_cache8_rows<HD, 4, true>), grid, dim3(256), 0, s, a);
   }
-  launch((k_cache8_attn<HD, kWaves, true>), dim3((uint32_t)(items * a.splits)), dim3(64 * kWaves), 0, s, a);
-  launch((k_cache8_join<HD>), dim3((uint32_t)((items * 16 * (HD / 4) + 255) / 256)), dim3(256), 0, s, a);
+  if (a.splits > 1)
+    launch((k_cache8_join<HD>), dim3((uint32_t)((items * rows * (HD / 4) + 255) / 256)), dim3(256), 0, s, a, rows);
   return hipGetLastError();
 }
 
@@ -455,13 +859,15 @@ hipError_t launch_cache8_attention(const Cache8& c, int heads, const Segs& rows,
                                    size_t ws_bytes, hipStream_t s) {
   Plan pl = plan(c, heads, rows, len);
   while (pl.splits > 1 && pl.bytes(c) > ws_bytes) --pl.splits;
-  const int64_t slots = (int64_t)pl.splits * pl.tiles.off[rows.B] * c.kv_heads * 16;
-  Attn8Args a{c, len, rows, pl.tiles, (const bf16*)q, (bf16*)o, ldq, ldo, heads / c.kv_heads, causal, pl.splits,
+  const int64_t slots = (int64_t)pl.splits * pl.tiles.off[rows.B] * c.kv_heads * pl.rows;
+  Lens held = len;
+  if (!c.n_pages) held = Lens{};                   // no pages: no tokens
+  Attn8Args a{c, held, rows, pl.tiles, (const bf16*)q, (bf16*)o, ldq, ldo, heads / c.kv_heads, causal, pl.splits,
               q_scaled ? 1.0f : attention_q_scale(c.hd), (float*)ws, (float*)ws + slots * c.hd};
   switch (c.hd) {
-    case 32: return launch_attn8<32>(a, s);
-    case 64: return launch_attn8<64>(a, s);
-    case 128: return launch_attn8<128>(a, s);
+    case 32: return launch_attn8<32>(a, pl.rows, s);
+    case 64: return launch_attn8<64>(a, pl.rows, s);
+    case 128: return launch_attn8<128>(a, pl.rows, s);
   }
   return hipErrorInvalidValue;
 }
