@@ -375,25 +375,34 @@ __device__ __forceinline__ void static_for(F f) {
   static_for_seq(f, std::make_integer_sequence<int, N>{});
 }
 
-// The largest of a tile's 16 scores: dependent v_max3 in one block (fmaxf would quiet each
-// operand first). NaN is passed over; its probability is NaN all the same.
+// The largest of a tile's 16 scores, in dependent v_max3 (fmaxf would quiet each operand
+// first). The first step is a builtin, for which the compiler waits until the matrix
+// core has written the tile; it does not for what inline assembly reads. NaN is passed over
+// (or makes the maximum infinite); its row is NaN all the same.
 __device__ __forceinline__ float max16(const f32x16& v) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3\n\t"
-      "v_max3_f32 %0, %0, %4, %5\n\t"
-      "v_max3_f32 %0, %0, %6, %7\n\t"
-      "v_max3_f32 %0, %0, %8, %9\n\t"
-      "v_max3_f32 %0, %0, %10, %11\n\t"
-      "v_max3_f32 %0, %0, %12, %13\n\t"
-      "v_max3_f32 %0, %0, %14, %15\n\t"
-      "v_max_f32 %0, %0, %16"
-      : "=&v"(r)
-      : "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]), "v"(v[8]), "v"(v[9]),
-        "v"(v[10]), "v"(v[11]), "v"(v[12]), "v"(v[13]), "v"(v[14]), "v"(v[15]));
+  float r = __builtin_amdgcn_fmed3f(v[0], v[1], INFINITY);
+  asm("v_max3_f32 %0, %0, %1, %2\n\t"
+      "v_max3_f32 %0, %0, %3, %4\n\t"
+      "v_max3_f32 %0, %0, %5, %6\n\t"
+      "v_max3_f32 %0, %0, %7, %8\n\t"
+      "v_max3_f32 %0, %0, %9, %10\n\t"
+      "v_max3_f32 %0, %0, %11, %12\n\t"
+      "v_max3_f32 %0, %0, %13, %14"
+      : "+&v"(r)
+      : "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]), "v"(v[8]), "v"(v[9]), "v"(v[10]), "v"(v[11]),
+        "v"(v[12]), "v"(v[13]), "v"(v[14]), "v"(v[15]));
   return r;
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// What is read in place of a page that is none: zeros.
+__device__ const u32x4 kNoPage[64] = {};
 
 // Many rows: NW waves of 32 rows each share a page, which goes to LDS by DMA as it
 // is, STAGES deep, its 16-byte chunks swizzled by row for conflict-free fragment reads;
@@ -424,7 +433,13 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
   const int b = find_segment_wave(p.tiles.off, p.tiles.B, tile);
   const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
   const int row_t = (tile - p.tiles.off[b]) * ROWS, row_w = row_t + wave * 32;
-  const int row = row_w + r32, tok = row / p.group, qcol = (head * p.group + row - tok * p.group) * HD;
+  // A lane's row: its token and its columns (found anew for the output, not kept)
+  auto place = [&](int lane_row, int& tok, int& col) {
+    tok = (row_w + lane_row) / p.group;
+    col = (head * p.group + row_w + lane_row - tok * p.group) * HD;
+  };
+  int tok, qcol;
+  place(r32, tok, qcol);
   const int lim = tok >= nq ? 0 : p.causal ? max(min(n, n - nq + tok + 1), 0) : n;
   // the wave's lowest limit, its highest, the workgroup's highest
   const int lim_lo = p.causal ? n - nq + row_w / p.group + 1 : n;
@@ -492,13 +507,14 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
   auto lane_f = [](float v, int i) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
   };
-  auto fetch = [&](int i, int stage) {             // page i (of those looked up); no page: the pool's first, unused
-    const int page = max(__builtin_amdgcn_readlane(pg, i - base), 0);
+  auto fetch = [&](int i, int stage) {             // page i (of those looked up)
+    const int page = __builtin_amdgcn_readlane(pg, i - base);
     const int64_t at = ((int64_t)page * kvh + head) * TILE;
 #pragma unroll
     for (int q = 0; q < DQ; ++q) {
       const int blk = wave + NW * q, of = blk < DMA ? blk : blk - DMA;
-      const uint8_t* from = (blk < DMA ? p.c.k : p.c.v) + at + of * 1024;
+      const uint8_t* from = page < 0 ? reinterpret_cast<const uint8_t*>(kNoPage)
+                                     : (blk < DMA ? p.c.k : p.c.v) + at + of * 1024;
       const uint32_t to = lds0 + (uint32_t)(stage * 2 * TILE + blk * 1024);
       asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(blk < DMA ? kdma : vdma), "s"(from), "{m0}"(to) : "memory");
     }
@@ -597,67 +613,59 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     }
   };
 
-  // A half step: scores `next` of half KH of the page at `kat`, probabilities pc of `cur`, the
-  // product of pp with half VH of the page at `vat`.
-  u32x4 kr[2];                                     // raw fragments of K (a pair of slices each)
-  u32x2 vr[2][2];                                  // and of V (an output tile each)
-  auto product_v = [&](uint32_t vat, int h, float vs, bf16x8 (&pp)[2]) __attribute__((always_inline)) {
+  // Half step: scores `next` of the 32 keys at `kat`, probabilities pc of `cur` (against the
+  // reference -ref), the product of pp with the 32 tokens of V at `vat`.
+  auto product_v = [&](uint32_t vat, float vs, const u32x4 (&pp)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < NV; ++t) {
-      const u32x2 a = read_v(vat, h, t, 0), c = read_v(vat, h, t, 1);
+      const u32x2 a = read_v(vat, 0, t, 0), c = read_v(vat, 0, t, 1);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const bf16x8 vf = widen8(a[u], c[u], vs);
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pp[u], o[t], 0, 0, 0);
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pp[u]), o[t], 0, 0, 0);
       }
       fence();
     }
-    pp[0] = pp[1] = bf16x8{};
   };
-  auto half_step = [&](auto hc, uint32_t kat, float ks, uint32_t vat, float vs, const f32x16& cur,
-                       f32x16& next, bf16x8 (&pp)[2], bf16x8 (&pc)[2]) __attribute__((always_inline)) {
-    constexpr int KH = decltype(hc)::value, VH = KH;                   // (i, 0): K of (i, 1), V of (i - 1, 1); ...
-    const float mx = half_max(max16(cur));
-    if (__any(mx > above)) {                       // rare
-      product_v(vat, VH, vs, pp);
-      rescale(fmaxf(m, mx * p.scale));
-    }
+  auto half_step = [&](uint32_t kat, float ks, uint32_t vat, float vs, float ref, const f32x16& cur, f32x16& next,
+                       const u32x4 (&pp)[2], u32x4 (&pc)[2]) __attribute__((always_inline)) {
     constexpr int G = 4 * NS, N = 16;              // groups of a product, K and V in turn; probabilities
+    u32x4 kr[2];                                   // raw fragments of K (a pair of slices each)
+    u32x2 vr[2][2];                                // and of V (an output tile each)
     float ex[N];
-    bf16x8 kf, vf;
-    kr[0] = read_k(kat, KH, 0);
-    vr[0][0] = read_v(vat, VH, 0, 0);
-    vr[0][1] = read_v(vat, VH, 0, 1);
+    kr[0] = read_k(kat, 0, 0);
+    vr[0][0] = read_v(vat, 0, 0, 0);
+    vr[0][1] = read_v(vat, 0, 0, 1);
     static_for<G>([&](auto nc) {
       constexpr int x = decltype(nc)::value, a = x / 2;
       if constexpr (x % 4 == 0 && x + 4 < G) {
-        kr[(a / 2 + 1) % 2] = read_k(kat, KH, a / 2 + 1);
-        vr[(a / 2 + 1) % 2][0] = read_v(vat, VH, a / 2 + 1, 0);
-        vr[(a / 2 + 1) % 2][1] = read_v(vat, VH, a / 2 + 1, 1);
+        kr[(a / 2 + 1) % 2] = read_k(kat, 0, a / 2 + 1);
+        vr[(a / 2 + 1) % 2][0] = read_v(vat, 0, a / 2 + 1, 0);
+        vr[(a / 2 + 1) % 2][1] = read_v(vat, 0, a / 2 + 1, 1);
       }
       if constexpr (x % 2 == 0) {
-        kf = widen8(kr[a / 2 % 2][2 * (a % 2)], kr[a / 2 % 2][2 * (a % 2) + 1], ks);
+        const bf16x8 kf = widen8(kr[a / 2 % 2][2 * (a % 2)], kr[a / 2 % 2][2 * (a % 2) + 1], ks);
         next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[a], a ? next : zero, 0, 0, 0);
       } else {
-        vf = widen8(vr[a / 2 % 2][0][a % 2], vr[a / 2 % 2][1][a % 2], vs);
-        o[a / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pp[a % 2], o[a / 2], 0, 0, 0);
+        const bf16x8 vf = widen8(vr[a / 2 % 2][0][a % 2], vr[a / 2 % 2][1][a % 2], vs);
+        o[a / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pp[a % 2]), o[a / 2], 0, 0, 0);
       }
-      constexpr int E0 = x * N / G, E1 = (x + 1) * N / G;
+      // exponentials, converted a group later
+      constexpr int E0 = x * N / G, E1 = (x + 1) * N / G, C0 = x ? (x - 1) * N / G & ~1 : 0,
+                    C1 = x + 1 == G ? N : E0 & ~1;
       static_for<E1 - E0>([&](auto k) {
         constexpr int i = E0 + decltype(k)::value;
-        ex[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[i], p.scale, -m));
-        if constexpr (i % 2) {
-          pc[i / 8][i % 8 - 1] = (bf16)ex[i - 1];
-          pc[i / 8][i % 8] = (bf16)ex[i];
-        }
-        if constexpr (i % 8 == 7) l = row_sum(pc[i / 8], l);
+        ex[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[i], p.scale, ref));
+      });
+      static_for<(C1 - C0) / 2>([&](auto k) {
+        constexpr int i = C0 + 2 * decltype(k)::value;
+        pc[i / 8][i / 2 % 4] = pack2(ex[i], ex[i + 1]);
+        if constexpr (i % 8 == 6) l = row_sum(__builtin_bit_cast(bf16x8, pc[i / 8]), l);
       });
       fence();
     });
   };
 
-  const std::integral_constant<int, 0> h0{};
-  const std::integral_constant<int, 1> h1{};
   for (int first = begin; first < end; first += 64) {
     const int last = min(first + 64, end);
     __syncthreads();                               // every wave past its reads of the last stages
@@ -665,62 +673,87 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     wait_vm<0>();
 #pragma unroll
     for (int i = 0; i < STAGES - 2; ++i) fetch(min(first + i, last - 1), i);
+    wait_vm<(STAGES - 3) * DQ>();
+    __builtin_amdgcn_s_barrier();                  // the first page has landed
+    fence();
     int stage = 0;                                 // of page i
-    auto sync = [&](int i) {                       // page i + 1 has landed (and i), the stage of i - 2 is free
+    auto sync = [&](int i) {                       // page i + 1 has landed, the stage of i - 2 is free
       wait_vm<(STAGES - 4) * DQ>();
       __builtin_amdgcn_s_barrier();
       fence();
       fetch(min(i + STAGES - 2, last - 1), stage >= 2 ? stage - 2 : stage + STAGES - 2);
     };
-    auto page_of = [&](int i) { return __builtin_amdgcn_readlane(pg, i - base); };
-    auto full = [&](int i) { return page_of(i) >= 0 && (i + 1) * kPage <= lim_lo; };
-    auto advance = [&] {
-      const uint32_t at = (uint32_t)(stage * 2 * TILE);
-      stage = stage == STAGES - 1 ? 0 : stage + 1;
-      return at;
-    };
-    int i = first;
-    while (i < last) {
-      if (!full(i)) {
-        sync(i);
-        const uint32_t at = advance();
-        if (page_of(i) >= 0 && i * kPage < lim_w) masked_page(i, at, lane_f(pks, i - base), lane_f(pvs, i - base));
-        ++i;
-        continue;
-      }
-      // A run of whole pages. In front of its first half step the probabilities before are
-      // zeros, times V of its first page, which every row sees.
+    auto none = [&](int i) { return __builtin_amdgcn_readlane(pg, i - base) < 0; };
+    auto at_stage = [&](int s) { return (uint32_t)(s * 2 * TILE); };
+    auto after = [&](int s) { return s == STAGES - 1 ? 0 : s + 1; };
+    // Pages that all of the wave's rows see, in half steps. A segment of them ends where a score
+    // calls for a move of the reference (a branch within the loop would copy the outputs
+    // at every step): it starts with scores of its own and no probabilities before them.
+    const int whole = row_w >= nq * p.group ? first : min(max(lim_lo / kPage, first), last);
+    int t = 2 * first;
+    while (t < 2 * whole) {
       f32x16 s0, s1;
-      bf16x8 p0[2], p1[2];
-      sync(i);
-      uint32_t at = advance(), at_before = at;
-      float ks = lane_f(pks, i - base), vs = lane_f(pvs, i - base), vs_before = vs;
-      p1[0] = p1[1] = bf16x8{};
+      u32x4 p0[2], p1[2];                          // (pairs, as bf16)
+      p1[0] = p1[1] = u32x4{0, 0, 0, 0};
+      int i = t / 2;
+      uint32_t vat = at_stage(stage) + (uint32_t)(8 * (t % 2));      // (zeros times V of this page, which every row sees)
+      float vsb = lane_f(pvs, i - base);
+      {
+        const uint32_t kat = at_stage(stage) + (uint32_t)(32 * HD * (t % 2));
+        const float ks = lane_f(pks, i - base);
 #pragma unroll
-      for (int x = 0; x < NS; ++x) {
-        const u32x4 w = read_k(at, 0, x);
-        const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
-        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * x], x ? s0 : zero, 0, 0, 0);
-        s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[2 * x + 1], s0, 0, 0, 0);
-        fence();
+        for (int x = 0; x < NS; ++x) {
+          const u32x4 w = read_k(kat, 0, x);
+          const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
+          s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * x], x ? s0 : zero, 0, 0, 0);
+          s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[2 * x + 1], s0, 0, 0, 0);
+          fence();
+        }
+        const float mx = half_max(max16(s0));
+        if (!none(i) && __any(mx > above)) rescale(fmaxf(m, mx * p.scale));
       }
-      for (;;) {
-        const int ahead = min(i + 1, last - 1) - base;
-        const float ks_next = lane_f(pks, ahead), vs_next = lane_f(pvs, ahead);
-        half_step(h1, at, ks, at_before, vs_before, s0, s1, p1, p0);
-        half_step(h0, (uint32_t)(stage * 2 * TILE), ks_next, at, vs, s1, s0, p0, p1);
-        at_before = at, vs_before = vs;
-        ++i;
-        if (i >= last || !full(i)) break;
-        sync(i);
-        at = advance();
-        ks = ks_next, vs = vs_next;
-      }
-      product_v(at_before, 1, vs_before, p1);
+      // A half step at t, then whether the segment ends. Where it has ended already (behind the
+      // first of a pair: the loop has one exit, or the outputs would be copied at it), it is
+      // no step: the product with pp and no probabilities.
+      bool done = false;
+      auto step = [&](const f32x16& cur, f32x16& next, const u32x4 (&pp)[2], u32x4 (&pc)[2])
+                      __attribute__((always_inline)) {
+        const bool second = t % 2;
+        if (!done && !second) sync(i);
+        // (behind the last half step scores of this page again: the next one may hold NaN that not
+        // all rows see, which no step may take)
+        const bool next_page = second && t + 1 < 2 * whole;
+        const int nx = next_page ? i + 1 : i;
+        const uint32_t here = at_stage(stage), kat = next_page ? at_stage(after(stage)) : here + 32 * HD;
+        // (a page that is none: its scores are 0 and its probabilities 0)
+        half_step(kat, lane_f(pks, nx - base), vat, vsb, done || none(i) ? -INFINITY : -m, cur, next, pp, pc);
+        if (!done) {
+          vat = here + (uint32_t)(8 * (t % 2));
+          vsb = lane_f(pvs, i - base);
+          done = t + 1 == 2 * whole;
+          if (second) ++i, stage = after(stage);
+          ++t;
+        }
+        done = done || (!none(i) && __any(half_max(max16(next)) > above));
+      };
+      do {
+        step(s0, s1, p1, p0);
+        step(s1, s0, p0, p1);
+      } while (!done);
+      product_v(vat, vsb, p1);
+    }
+    for (int i = whole; i < last; ++i) {
+      sync(i);
+      const uint32_t at = at_stage(stage);
+      stage = after(stage);
+      if (!none(i) && i * kPage < lim_w) masked_page(i, at, lane_f(pks, i - base), lane_f(pvs, i - base));
     }
   }
   wait_vm<0>();                                    // no DMA into LDS that another workgroup may get
   const float sum = half_sum(l[0]);
+  int again = r32;
+  asm("" : "+v"(again));
+  place(again, tok, qcol);
   if constexpr (SPLIT) {
     const int64_t slot = (((int64_t)split * n_tiles + tile) * kvh + head) * ROWS + wave * 32 + r32;
 #pragma unroll
