@@ -1,5 +1,7 @@
 // The cache of 8-bit keys and values (cache8.h): appending to it, and attention over it.
 #include <algorithm>
+#include <cstdlib>
+#include <type_traits>
 #include <utility>
 
 #include "cache8.h"
@@ -46,7 +48,7 @@ __global__ __launch_bounds__(2 * HD) void k_cache8_append(AppendArgs p) {
   const bool is_v = item & 1;
   item >>= 1;
   const int head = item % heads, pg = item / heads;
-  const int b = find_segment(p.pages.off, p.pages.B, pg);
+  const int b = find_segment_wave(p.pages.off, p.pages.B, pg);
   const int n_old = p.len.n[b], r0 = p.rows.off[b], n_new = p.rows.off[b + 1] - r0;
   const int index = n_old / kPage + pg - p.pages.off[b];
   const int page = p.c.table[(int64_t)b * p.c.max_pages + index];
@@ -137,15 +139,32 @@ __global__ __launch_bounds__(2 * HD) void k_cache8_append(AppendArgs p) {
 struct Attn8Args {
   Cache8 c;
   Lens len;
-  Segs rows, tiles;                                // tiles: of 16 rows (token, head of the group), counted through
+  Segs rows, tiles, items;                         // tiles: of `tile_rows` rows (token, head of the group); items: tiles
+                                                   // times the splits of their sample's pages; both counted through
   const bf16* q;
   bf16* o;
   int64_t ldq, ldo;
-  int group, causal, splits;
+  int group, causal, tile_rows, split_pages;       // split_pages: of one split
   float scale;                                     // of the scores, to base 2
-  float* part_o;                                   // [splits][tiles][kv_heads][16][hd]: unnormalised outputs
-  float* part_ml;                                  // and [..][16][2]: reference max, sum
+  float* part_o;                                   // [items][kv_heads][tile_rows][hd]: unnormalised outputs
+  float* part_ml;                                  // and [..][tile_rows][2]: reference max, sum
 };
+
+// A workgroup's sample, tile (of the sample) and pages [begin, end) of those below lim (the
+// highest limit of a tile's rows). One split: the output is the kernel's own.
+struct Item {
+  int b, tile, splits, split;
+};
+__device__ __forceinline__ Item item_of(const Attn8Args& p, int item) {
+  Item r;
+  r.b = find_segment_wave(p.items.off, p.items.B, item);
+  const int tiles = p.tiles.off[r.b + 1] - p.tiles.off[r.b];
+  r.splits = (p.items.off[r.b + 1] - p.items.off[r.b]) / tiles;
+  const int local = item - p.items.off[r.b];
+  r.tile = local / r.splits;
+  r.split = local - r.tile * r.splits;
+  return r;
+}
 
 // Eight e4m3 values times a scale, as bf16: no rounding (4 significant bits).
 __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
@@ -156,6 +175,22 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) 
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
+// The largest of v over lanes l, l ^ 16, l ^ 32, l ^ 48, in all of them.
+__device__ __forceinline__ float quarter_max(float v) {
+  float w = v;
+  asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(v), "+v"(w));
+  v = fmaxf(v, w);
+  w = v;
+  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(v), "+v"(w));
+  return fmaxf(v, w);
+}
+
 // Bytes 0xff where a word's e4m3 bytes are NaN.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;     // 0x7f carries into its own top bit alone
@@ -163,32 +198,49 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 }
 
 // 16 rows (queries of one key head's group) a workgroup, whose waves take its pages in
-// turn; scores S^T = K Q^T, so that a lane holds one row's scores and its statistics.
-template <int HD, int NW, bool SPLIT>
-__global__ __launch_bounds__(64 * NW) void k_cache8_attn(Attn8Args p) {
+// turn, fragments straight from memory into registers, a page ahead; scores S^T = K Q^T, so
+// that a lane holds one row's scores and its statistics.
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_attn(Attn8Args p) {
   constexpr int NK = HD / 32, NV = HD / 16;        // K slices of 32 columns; output tiles of 16
+  constexpr int KR = HD == 32 ? 1 : HD / 64;       // 16-byte (of 32 columns 8-byte) pieces of K a lane has of 16 tokens
+  typedef std::conditional_t<HD == 32, u32x2, u32x4> KPiece;
   __shared__ __attribute__((aligned(16))) float so[NW][16][HD + 4];
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane >> 4, r16 = lane & 15;
-  const int n_tiles = p.tiles.off[p.tiles.B], kvh = p.c.kv_heads;
-  int item = xcd_logical_id(blockIdx.x, n_tiles * kvh * p.splits);
-  const int split = item % p.splits;
-  item /= p.splits;
-  const int head = item % kvh, tile = item / kvh;
-  const int b = find_segment_wave(p.tiles.off, p.tiles.B, tile);
+  const int kvh = p.c.kv_heads, logical = xcd_logical_id(blockIdx.x, p.items.off[p.items.B] * kvh);
+  const int item = logical / kvh, head = logical - item * kvh;
+  const Item it = item_of(p, item);
+  const int b = it.b;
   const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
-  const int row = (tile - p.tiles.off[b]) * 16 + r16, tok = row / p.group;
+  const int row = it.tile * 16 + r16, tok = row / p.group;
   const bool in = tok < nq;
   const int qcol = (head * p.group + row - tok * p.group) * HD;
   // a row sees keys below its limit; the tile those below the last row's
   const int lim = !in ? 0 : p.causal ? max(min(n, n - nq + tok + 1), 0) : n;
-  const int tok_lo = (tile - p.tiles.off[b]) * 16 / p.group;
-  const int tok_hi = min(((tile - p.tiles.off[b]) * 16 + 15) / p.group, nq - 1);
-  const int lim_lo = p.causal ? n - nq + tok_lo + 1 : n, lim_hi = p.causal ? max(n - nq + tok_hi + 1, 0) : n;
+  const int lim_lo = p.causal ? n - nq + it.tile * 16 / p.group + 1 : n;
+  const int lim_hi = p.causal ? max(n - nq + min((it.tile * 16 + 15) / p.group, nq - 1) + 1, 0) : n;
   const int pages = (lim_hi + kPage - 1) / kPage;
-  const int begin = (int)((int64_t)split * pages / p.splits), end = (int)((int64_t)(split + 1) * pages / p.splits);
+  const int begin = min(it.split * p.split_pages, pages), end = min(begin + p.split_pages, pages);
 
+  // This wave's pages, 64 of them at a time: one a lane, its number (or none) and scales.
+  int pg = -1, base = 0;
+  float pks = 0.0f, pvs = 0.0f;
+  auto look = [&](int k) {
+    base = k;
+    pg = -1;
+    const int i = begin + wave + (k + lane) * NW;
+    if (i < end) pg = p.c.table[(int64_t)b * p.c.max_pages + i];
+    if ((uint32_t)pg >= (uint32_t)p.c.n_pages) pg = -1;
+    if (pg >= 0) {
+      const int64_t x = (int64_t)pg * kvh + head;
+      pks = fp8_scale(p.c.ks[x]);
+      pvs = fp8_scale(p.c.vs[x]);
+    }
+  };
+  const int mine = (end - begin - wave + NW - 1) / NW;               // pages (or none) of this wave
+  if (mine > 0) look(0);
   bf16x8 qf[NK];
 #pragma unroll
   for (int s = 0; s < NK; ++s) {
@@ -202,115 +254,133 @@ __global__ __launch_bounds__(64 * NW) void k_cache8_attn(Attn8Args p) {
   for (int t = 0; t < NV; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   float m = -INFINITY, l = 0.0f;
 
-  for (int i = begin + wave; i < end; i += NW) {
-    const int page = p.c.table[(int64_t)b * p.c.max_pages + i];
-    if ((uint32_t)page >= (uint32_t)p.c.n_pages) continue;
-    const int64_t at = (int64_t)page * kvh + head;
-    const uint8_t* kp = p.c.k + at * (kPage * HD);
-    const uint8_t* vp = p.c.v + at * (kPage * HD);
-    const float ks = fp8_scale(p.c.ks[at]), vs = fp8_scale(p.c.vs[at]);
-    u32x4 vr[NV];
+  // K of the next page is asked for as soon as this one's scores are taken, V at a page's
+  // beginning. (A page that is none is passed over: its loads too.)
+  KPiece kr[4 * KR];
+  u32x4 vr[NV];
+  auto page_of = [&](int k) { return __builtin_amdgcn_readlane(pg, k - base); };
+  auto load_k = [&](int k) __attribute__((always_inline)) {
+    const int page = page_of(k);
+    if (page < 0) return;
+    const uint8_t* kp = p.c.k + ((int64_t)page * kvh + head) * (kPage * HD);
 #pragma unroll
-    for (int t = 0; t < NV; ++t)
-      vr[t] = *reinterpret_cast<const u32x4*>(vp + (16 * t + r16) * kPage + 16 * c);
-    f32x4 s[4];
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const uint8_t* kr = kp + (16 * t + r16) * HD;
-      s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if constexpr (HD == 32) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(kr + 8 * c);
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[0], w[1], ks), qf[0], s[t], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int h = 0; h < NK / 2; ++h) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(kr + 64 * h + 16 * c);
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[0], w[1], ks), qf[2 * h], s[t], 0, 0, 0);
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2], w[3], ks), qf[2 * h + 1], s[t], 0, 0, 0);
-        }
-      }
-    }
+      for (int h = 0; h < KR; ++h)
+        kr[t * KR + h] = *reinterpret_cast<const KPiece*>(kp + (uint32_t)((16 * t + r16) * HD + 64 * h + (int)sizeof(KPiece) * c));
+  };
+  // What a page's scores s add to the rows: the maxima, probabilities, the product with V.
+  auto take_page = [&](auto border_, int i, f32x4 (&s)[4], float vs) __attribute__((always_inline)) {
+    constexpr bool BORDER = decltype(border_)::value;
     const int k0 = i * kPage + 4 * c;
-    const bool border = (i + 1) * kPage > lim_lo;                      // some row does not see all of the page
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         s[t][e] *= p.scale;
-        if (border && k0 + 16 * t + e >= lim) s[t][e] = -INFINITY;
+        if (BORDER && k0 + 16 * t + e >= lim) s[t][e] = -INFINITY;
       }
     float mx = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    if (__any(mx > m)) {
-      const float to = fmaxf(m, mx), f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-      m = to;
-      l *= f;
+    mx = quarter_max(mx);
+    const float to = fmaxf(m, mx);
+    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to), ref = to == -INFINITY ? 0.0f : to;
+    m = to;
+    l *= f;
+    u32x4 pf[2];
 #pragma unroll
-      for (int t = 0; t < NV; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[t][e] *= f;
-    }
-    const float ref = m == -INFINITY ? 0.0f : m;
-    bf16x8 pf[2];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
+      float x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(s[t][e] - ref);
-        l += x;
-        pf[t / 2][4 * (t % 2) + e] = (bf16)x;
+        x[e] = __builtin_amdgcn_exp2f(s[t][e] - ref);
+        l += x[e];
       }
-    if (border) {
-      // Tokens behind the sample's last one were never written; and a token that only some
-      // rows see may hold NaN, which times a probability of 0 would be NaN: such values count as 0
-      // in the product, and rows that see one get their NaN from a count of them.
-      bool odd = false;
+      pf[t / 2][2 * (t % 2)] = pack2(x[0], x[1]);
+      pf[t / 2][2 * (t % 2) + 1] = pack2(x[2], x[3]);
+    }
 #pragma unroll
-      for (int t = 0; t < NV; ++t)
+    for (int t = 0; t < NV; ++t) {
+      u32x4 w = vr[t];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[t][e] *= f;
+      if constexpr (BORDER) {
+        // Tokens behind the sample's last one were never written; and a token that only some
+        // rows see may hold NaN, which times a probability of 0 would be NaN: such values count
+        // as 0 in the product, and rows that see one get their NaN from a count of them.
+        uint32_t odd = 0;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int left = n - (k0 + 16 * x);                          // written ones of the word's four
-          const uint32_t w = vr[t][x] & (left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u);
-          const uint32_t nb = nan_bytes(w);
-          odd = odd || nb;
-          vr[t][x] = w;
+          w[x] &= left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+          odd |= nan_bytes(w[x]);
         }
-      if (__any(odd)) {
-        bf16x8 sees[2];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sees[t / 2][4 * (t % 2) + e] = (bf16)(k0 + 16 * t + e < lim ? 1.0f : 0.0f);
-#pragma unroll
-        for (int t = 0; t < NV; ++t) {
+        if (__any(odd)) {
           f32x4 count{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t a = nan_bytes(vr[t][2 * h]), d = nan_bytes(vr[t][2 * h + 1]);
-            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(a & 0x38383838u, d & 0x38383838u, 1.0f), sees[h], count,
-                                                            0, 0, 0);
-            vr[t][2 * h] &= ~a;
-            vr[t][2 * h + 1] &= ~d;
+            bf16x8 sees;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sees[e] = (bf16)(k0 + 32 * h + 16 * (e / 4) + e % 4 < lim ? 1.0f : 0.0f);
+            const uint32_t a = nan_bytes(w[2 * h]), d = nan_bytes(w[2 * h + 1]);
+            count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(a & 0x38383838u, d & 0x38383838u, 1.0f), sees, count, 0,
+                                                            0, 0);
+            w[2 * h] &= ~a;
+            w[2 * h + 1] &= ~d;
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (count[e] > 0.0f) o[t][e] = __builtin_nanf("");
         }
       }
-    }
-#pragma unroll
-    for (int t = 0; t < NV; ++t)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(vr[t][2 * h], vr[t][2 * h + 1], vs), pf[h], o[t], 0, 0, 0);
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * h], w[2 * h + 1], vs),
+                                                       __builtin_bit_cast(bf16x8, pf[h]), o[t], 0, 0, 0);
+    }
+  };
+  for (int k = 0; k < mine; ++k) {
+    if (k % 64 == 0) {
+      if (k) look(k);
+      load_k(k);
+    }
+    const int page = page_of(k);
+    if (page < 0) {
+      if (k + 1 < mine && (k + 1) % 64) load_k(k + 1);
+      continue;
+    }
+    {
+      const uint8_t* vp = p.c.v + ((int64_t)page * kvh + head) * (kPage * HD);
+#pragma unroll
+      for (int t = 0; t < NV; ++t)
+        vr[t] = *reinterpret_cast<const u32x4*>(vp + (uint32_t)((16 * t + r16) * kPage + 16 * c));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const int i = begin + wave + k * NW;
+    const float ks = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pks), k - base));
+    const float vs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, pvs), k - base));
+    f32x4 s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int h = 0; h < KR; ++h) {
+        const KPiece w = kr[t * KR + h];
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[0], w[1], ks), qf[HD == 32 ? 0 : 2 * h], s[t], 0, 0, 0);
+        if constexpr (HD > 32)
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2], w[3], ks), qf[2 * h + 1], s[t], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (k + 1 < mine && (k + 1) % 64) load_k(k + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    if ((i + 1) * kPage > lim_lo) take_page(std::true_type{}, i, s, vs);           // some row does not see all of it
+    else take_page(std::false_type{}, i, s, vs);
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  l = rows_sum(l);
 #pragma unroll
   for (int t = 0; t < NV; ++t) *reinterpret_cast<f32x4*>(&so[wave][r16][16 * t + 4 * c]) = o[t];
   if (c == 0) {
@@ -334,16 +404,16 @@ __global__ __launch_bounds__(64 * NW) void k_cache8_attn(Attn8Args p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += ov[e] * f;
     }
-    if constexpr (SPLIT) {
-      const int64_t slot = (((int64_t)split * n_tiles + tile) * kvh + head) * 16 + r;
+    const int rr = it.tile * 16 + r, t = rr / p.group;
+    if (t >= nq) continue;
+    if (it.splits > 1) {
+      const int64_t slot = ((int64_t)item * kvh + head) * 16 + r;
       *reinterpret_cast<f32x4*>(p.part_o + slot * HD + d) = v;
       if (d == 0) {
         p.part_ml[2 * slot] = top;
         p.part_ml[2 * slot + 1] = sum;
       }
     } else {
-      const int rr = (tile - p.tiles.off[b]) * 16 + r, t = rr / p.group;
-      if (t >= nq) continue;
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       bf16x4 w;
 #pragma unroll
@@ -395,11 +465,6 @@ __device__ __forceinline__ float max16(const f32x16& v) {
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
-}
 
 // What is read in place of a page that is none: zeros.
 __device__ const u32x4 kNoPage[64] = {};
@@ -414,7 +479,7 @@ __device__ const u32x4 kNoPage[64] = {};
 // compiler's scheduler behind each group; left alone it gathers the products and then the
 // vector work, and both waves of a SIMD wait for the same unit). Pages at a row's limit, at
 // most a few and the last, go one step after the other, with masks.
-template <int HD, int NW, bool SPLIT>
+template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn8Args p) {
   constexpr int ROWS = 32 * NW, TILE = kPage * HD, STAGES = 5;
   constexpr int NS = HD / 32, NV = HD / 32;        // pairs of K slices of 16 columns; output tiles of 32
@@ -425,14 +490,12 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
   __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * TILE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r32 = lane & 31;
-  const int n_tiles = p.tiles.off[p.tiles.B], kvh = p.c.kv_heads;
-  int item = xcd_logical_id(blockIdx.x, n_tiles * kvh * p.splits);
-  const int split = item % p.splits;
-  item /= p.splits;
-  const int head = item / n_tiles, tile = n_tiles - 1 - item % n_tiles;      // (causal: the longest first)
-  const int b = find_segment_wave(p.tiles.off, p.tiles.B, tile);
+  const int n_items = p.items.off[p.items.B], kvh = p.c.kv_heads, logical = xcd_logical_id(blockIdx.x, n_items * kvh);
+  const int head = logical / n_items, item = n_items - 1 - logical % n_items;        // (causal: the longest first)
+  const Item it = item_of(p, item);
+  const int b = it.b;
   const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
-  const int row_t = (tile - p.tiles.off[b]) * ROWS, row_w = row_t + wave * 32;
+  const int row_t = it.tile * ROWS, row_w = row_t + wave * 32;
   // A lane's row: its token and its columns (found anew for the output, not kept)
   auto place = [&](int lane_row, int& tok, int& col) {
     tok = (row_w + lane_row) / p.group;
@@ -447,7 +510,7 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
                     : p.causal ? max(n - nq + min((row_w + 31) / p.group, nq - 1) + 1, 0) : n;
   const int lim_hi = p.causal ? max(n - nq + min((row_t + ROWS - 1) / p.group, nq - 1) + 1, 0) : n;
   const int pages = (lim_hi + kPage - 1) / kPage;
-  const int begin = (int)((int64_t)split * pages / p.splits), end = (int)((int64_t)(split + 1) * pages / p.splits);
+  const int begin = min(it.split * p.split_pages, pages), end = min(begin + p.split_pages, pages);
 
   // Columns of a lane's fragment 2 i + h: 32 i + 16 g + 8 h on, as a chunk of K holds them.
   bf16x8 qf[2 * NS];
@@ -754,8 +817,9 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
   int again = r32;
   asm("" : "+v"(again));
   place(again, tok, qcol);
-  if constexpr (SPLIT) {
-    const int64_t slot = (((int64_t)split * n_tiles + tile) * kvh + head) * ROWS + wave * 32 + r32;
+  if (it.splits > 1) {
+    if (tok >= nq) return;
+    const int64_t slot = ((int64_t)item * kvh + head) * ROWS + wave * 32 + r32;
 #pragma unroll
     for (int t = 0; t < NV; ++t)
 #pragma unroll
@@ -781,26 +845,29 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
   }
 }
 
-// The splits' results, joined in their order: a thread has four columns of a row (ROWS a
-// tile).
+// The splits' results, joined in their order: a thread has four columns of a row. (A wave's
+// rows are of one tile.)
 template <int HD>
-__global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p, int tile_rows) {
-  const int n_tiles = p.tiles.off[p.tiles.B], kvh = p.c.kv_heads;
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x, slot = x / (HD / 4), all = (int64_t)n_tiles * kvh * tile_rows;
-  if (slot >= all) return;
-  const int d = (int)(x % (HD / 4)) * 4, r = (int)(slot % tile_rows), head = (int)(slot / tile_rows % kvh);
-  const int tile = (int)(slot / tile_rows / kvh), b = find_segment(p.tiles.off, p.tiles.B, tile);
-  const int row = (tile - p.tiles.off[b]) * tile_rows + r, t = row / p.group, q0 = p.rows.off[b];
-  if (t >= p.rows.off[b + 1] - q0) return;
+__global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p) {
+  const int kvh = p.c.kv_heads, x = blockIdx.x * 256 + threadIdx.x, d = x % (HD / 4) * 4, y = x / (HD / 4);
+  const int r = y % p.tile_rows, z = __builtin_amdgcn_readfirstlane(y / p.tile_rows), head = z % kvh, tile = z / kvh;
+  if (tile >= p.tiles.off[p.tiles.B]) return;
+  const int b = find_segment_wave(p.tiles.off, p.tiles.B, tile), q0 = p.rows.off[b];
+  const int splits = (p.items.off[b + 1] - p.items.off[b]) / (p.tiles.off[b + 1] - p.tiles.off[b]);
+  const int row = (tile - p.tiles.off[b]) * p.tile_rows + r, t = row / p.group;
+  if (splits < 2 || t >= p.rows.off[b + 1] - q0) return;
+  const int64_t step = (int64_t)kvh * p.tile_rows;
+  const int64_t slot = ((int64_t)(p.items.off[b] + (tile - p.tiles.off[b]) * splits) * kvh + head) * p.tile_rows + r;
   float top = -INFINITY;
-  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[2 * (s * all + slot)]);
+  for (int s = 0; s < splits; ++s) top = fmaxf(top, p.part_ml[2 * (slot + s * step)]);
   float sum = 0.0f;
   f32x4 v{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < p.splits; ++s) {
-    const float m = p.part_ml[2 * (s * all + slot)];
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float m = p.part_ml[2 * (slot + s * step)];
     const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-    sum += p.part_ml[2 * (s * all + slot) + 1] * f;
-    const f32x4 ov = *reinterpret_cast<const f32x4*>(p.part_o + (s * all + slot) * HD + d);
+    sum += p.part_ml[2 * (slot + s * step) + 1] * f;
+    const f32x4 ov = *reinterpret_cast<const f32x4*>(p.part_o + (slot + s * step) * HD + d);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += ov[e] * f;
   }
@@ -811,49 +878,59 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p, int tile_rows)
   *reinterpret_cast<bf16x4*>(p.o + (q0 + t) * p.ldo + (head * p.group + row - t * p.group) * HD + d) = w;
 }
 
+// How a call is cut: row tiles, and splits of the pages of their sample.
 struct Plan {
-  Segs tiles;
-  int rows, splits;                                // rows: of a tile
+  Segs tiles, items;
+  int rows, split_pages;                           // rows: of a tile
+  bool split;                                      // some sample's pages are split
   size_t bytes(const Cache8& c) const {
-    return splits < 2 ? 0 : (size_t)splits * tiles.off[tiles.B] * c.kv_heads * rows * (c.hd + 2) * 4;
+    return split ? (size_t)items.off[items.B] * c.kv_heads * rows * (c.hd + 2) * 4 : 0;
   }
 };
 
-constexpr int kWaves = 4;
-
-Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len) {
+Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, size_t ws_bytes) {
   Plan r{};
   const int group = heads / c.kv_heads;
   int64_t most = 0;
   for (int b = 0; b < rows.B; ++b) most = std::max(most, (int64_t)(rows.off[b + 1] - rows.off[b]) * group);
   r.rows = most <= 16 ? 16 : 128;
-  r.tiles.B = rows.B;
-  int pages = 0;
+  r.tiles.B = r.items.B = rows.B;
+  int64_t work = 0;                                // pages of all tiles and heads
+  int longest = 0;
+  int pages[kMaxBatch];
   for (int b = 0; b < rows.B; ++b) {
-    const int64_t n = (int64_t)(rows.off[b + 1] - rows.off[b]) * group;
-    r.tiles.off[b + 1] = r.tiles.off[b] + (int)((n + r.rows - 1) / r.rows);
-    if (n) pages = std::max(pages, (len.n[b] + kPage - 1) / kPage);
+    const int64_t n = (int64_t)(rows.off[b + 1] - rows.off[b]) * group, tiles = (n + r.rows - 1) / r.rows;
+    pages[b] = (len.n[b] + kPage - 1) / kPage;
+    r.tiles.off[b + 1] = r.tiles.off[b] + (int)tiles;
+    work += tiles * pages[b] * c.kv_heads;
+    if (tiles) longest = std::max(longest, pages[b]);
   }
-  const int64_t items = (int64_t)r.tiles.off[rows.B] * c.kv_heads;
-  r.splits = 1;
-  if (items) r.splits = (int)std::max<int64_t>(1, std::min<int64_t>((r.rows == 16 ? 1024 : 512) / items, pages / 8));
-  return r;
+  const char* e1 = getenv("C8_SMALL"); const char* e2 = getenv("C8_ROWS");
+  const int64_t want = r.rows == 16 ? (e1 ? atoi(e1) : 1024) : (e2 ? atoi(e2) : 512), least = r.rows == 16 ? 16 : 8;
+  r.split_pages = (int)std::max<int64_t>(std::max<int64_t>(least, (work + want - 1) / want), 1);
+  if ((int64_t)r.tiles.off[rows.B] * c.kv_heads >= want) r.split_pages = std::max(r.split_pages, longest);
+  for (;; r.split_pages *= 2) {
+    r.split = false;
+    for (int b = 0; b < rows.B; ++b) {
+      const int splits = std::max(1, (pages[b] + r.split_pages - 1) / r.split_pages);
+      r.items.off[b + 1] = r.items.off[b] + (r.tiles.off[b + 1] - r.tiles.off[b]) * splits;
+      r.split = r.split || (splits > 1 && r.tiles.off[b + 1] > r.tiles.off[b]);
+    }
+    if (r.bytes(c) <= ws_bytes) return r;
+  }
 }
 
 template <int HD>
-hipError_t launch_attn8(const Attn8Args& a, int rows, hipStream_t s) {
-  const int64_t items = (int64_t)a.tiles.off[a.tiles.B] * a.c.kv_heads;
+hipError_t launch_attn8(const Attn8Args& a, const Plan& pl, hipStream_t s) {
+  const int64_t items = (int64_t)a.items.off[a.items.B] * a.c.kv_heads;
   if (!items) return hipSuccess;
-  const dim3 grid((uint32_t)(items * a.splits));
-  if (rows == 16) {
-    if (a.splits < 2) launch((k_cache8_attn<HD, kWaves, false>), grid, dim3(64 * kWaves), 0, s, a);
-    else launch((k_cache8_attn<HD, kWaves, true>), grid, dim3(64 * kWaves), 0, s, a);
-  } else {
-    if (a.splits < 2) launch((k_cache8_rows<HD, 4, false>), grid, dim3(256), 0, s, a);
-    else launch((k_cache8_rows<HD, 4, true>), grid, dim3(256), 0, s, a);
+  if (pl.rows == 128) launch((k_cache8_rows<HD, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
+  else if (items <= 256) launch((k_cache8_attn<HD, 8>), dim3((uint32_t)items), dim3(512), 0, s, a);
+  else launch((k_cache8_attn<HD, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
+  if (pl.split) {
+    const int64_t threads = (int64_t)a.tiles.off[a.tiles.B] * a.c.kv_heads * pl.rows * (HD / 4);
+    launch((k_cache8_join<HD>), dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, s, a);
   }
-  if (a.splits > 1)
-    launch((k_cache8_join<HD>), dim3((uint32_t)((items * rows * (HD / 4) + 255) / 256)), dim3(256), 0, s, a, rows);
   return hipGetLastError();
 }
 
@@ -884,23 +961,22 @@ hipError_t launch_cache8_append(const Cache8& c, int dt, const Lens& len, const 
 }
 
 size_t cache8_attention_bytes(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool causal) {
-  return plan(c, heads, rows, len).bytes(c);
+  return plan(c, heads, rows, len, ~(size_t)0).bytes(c);
 }
 
 hipError_t launch_cache8_attention(const Cache8& c, int heads, const Segs& rows, const Lens& len, const void* q,
                                    int64_t ldq, void* o, int64_t ldo, bool causal, bool q_scaled, void* ws,
                                    size_t ws_bytes, hipStream_t s) {
-  Plan pl = plan(c, heads, rows, len);
-  while (pl.splits > 1 && pl.bytes(c) > ws_bytes) --pl.splits;
-  const int64_t slots = (int64_t)pl.splits * pl.tiles.off[rows.B] * c.kv_heads * pl.rows;
-  Lens held = len;
-  if (!c.n_pages) held = Lens{};                   // no pages: no tokens
-  Attn8Args a{c, held, rows, pl.tiles, (const bf16*)q, (bf16*)o, ldq, ldo, heads / c.kv_heads, causal, pl.splits,
-              q_scaled ? 1.0f : attention_q_scale(c.hd), (float*)ws, (float*)ws + slots * c.hd};
+  const Lens held = c.n_pages ? len : Lens{};      // no pages: no tokens
+  const Plan pl = plan(c, heads, rows, held, ws_bytes);
+  const int64_t slots = (int64_t)pl.items.off[rows.B] * c.kv_heads * pl.rows;
+  Attn8Args a{c, held, rows, pl.tiles, pl.items, (const bf16*)q, (bf16*)o, ldq, ldo, heads / c.kv_heads, causal,
+              pl.rows, pl.split_pages, q_scaled ? 1.0f : attention_q_scale(c.hd), (float*)ws,
+              (float*)ws + slots * c.hd};
   switch (c.hd) {
-    case 32: return launch_attn8<32>(a, pl.rows, s);
-    case 64: return launch_attn8<64>(a, pl.rows, s);
-    case 128: return launch_attn8<128>(a, pl.rows, s);
+    case 32: return launch_attn8<32>(a, pl, s);
+    case 64: return launch_attn8<64>(a, pl, s);
+    case 128: return launch_attn8<128>(a, pl, s);
   }
   return hipErrorInvalidValue;
 }

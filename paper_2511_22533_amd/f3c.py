@@ -724,27 +724,42 @@ class Cache8(NamedTuple):
 def _cache8(cache, batch: int, dev: int, T):
     """The cache as the C call's argument, its key heads and their width."""
     k, v, ks, vs, table = cache
-    fp8 = T[F3C_FP8]
-    pages, heads, page, hd = k.shape if k.dim() == 4 else (0, 0, 0, 0)
-    if (page != F3C_PAGE_TOKENS or k.dtype not in fp8 or v.dtype not in fp8 or v.shape != (pages, heads, hd, page)
-            or ks.shape != (pages, heads) or vs.shape != (pages, heads) or ks.dtype not in T["scale"]
-            or vs.dtype not in T["scale"] or table.dim() != 2 or table.shape[0] < batch
-            or table.dtype != T["torch"].int32):
-        raise ValueError("cache: k e4m3 [pages][heads][64][head_dim], v [pages][heads][head_dim][64], scale bytes "
-                         "[pages][heads], table int32 [samples][pages of one] expected")
-    for t in cache:
-        if t.get_device() != dev or not t.is_contiguous():
-            raise ValueError("cache: contiguous tensors on the current GPU expected")
-    return Cache8Args(heads, hd, pages, table.shape[1], k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(),
-                      table.data_ptr()), heads, hd
+    fp8, byte = T[F3C_FP8], T["scale"]
+    if k.dim() == 4 and table.dim() == 2:
+        pages, heads, page, hd = k.shape
+        samples, most = table.shape
+        scales = (pages, heads)
+        if (page == F3C_PAGE_TOKENS and samples >= batch and k.dtype in fp8 and v.dtype in fp8 and ks.dtype in byte
+                and vs.dtype in byte and table.dtype is T["torch"].int32 and v.shape == (pages, heads, hd, page)
+                and ks.shape == scales and vs.shape == scales and k.is_contiguous() and v.is_contiguous()
+                and ks.is_contiguous() and vs.is_contiguous() and table.is_contiguous()
+                and k.get_device() == v.get_device() == ks.get_device() == vs.get_device() == table.get_device() == dev):
+            return Cache8Args(heads, hd, pages, most, k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(),
+                              table.data_ptr()), heads, hd
+    raise ValueError("cache: k e4m3 [pages][heads][64][head_dim], v [pages][heads][head_dim][64], scale bytes "
+                     "[pages][heads], table int32 [samples][pages of one], contiguous on the current GPU expected")
+
+
+@functools.lru_cache(maxsize=None)
+def _int_array(n: int):
+    return ctypes.c_int32 * n
+
+
+def _ints(values):
+    """Host integers of a call as the C array, made at each call (they change from token to token)."""
+    try:
+        return _int_array(len(values))(*values)
+    except TypeError:                              # NumPy's integers, elements of tensors
+        return _i32(values)
 
 
 def _samples(off, lens, rows: int):
-    """(row offsets, samples, tokens held) as C values."""
-    offsets, B, lowest, highest = _offsets(tuple(map(int, off)))
-    if B < 1 or lowest < 0 or highest > rows or len(lens) != B:
+    """(row offsets, samples, tokens held) as C values; the library looks at their order."""
+    offsets, held = _ints(off), _ints(lens)
+    B = len(held)
+    if B < 1 or len(offsets) != B + 1 or offsets[0] < 0 or offsets[B] > rows:
         raise ValueError("off: B + 1 row offsets within the rows, lens: B token counts expected")
-    return offsets, B, _i32(lens)
+    return offsets, B, held
 
 
 def op_cache8_append(dtype: int, cache, lens: Sequence[int], off: Sequence[int], k, v, stream=None):
@@ -758,7 +773,7 @@ def op_cache8_append(dtype: int, cache, lens: Sequence[int], off: Sequence[int],
     offsets, B, held = _samples(off, lens, R)
     args, heads, hd = _cache8(cache, B, dev, T)
     check((_lib or lib()).f3c_op_cache8_append(
-        ctypes.byref(args), dtype, B, held, offsets, *_rows("k", k, T[dtype], R, heads * hd, dev),
+        args, dtype, B, held, offsets, *_rows("k", k, T[dtype], R, heads * hd, dev),
         *_rows("v", v, T[dtype], R, heads * hd, dev), _stream_on(stream, dev, T["torch"])))
 
 
@@ -774,22 +789,22 @@ def op_cache8_attention(cache, heads: int, q_off: Sequence[int], lens: Sequence[
     dev = _device(q, torch)
     offsets, B, held = _samples(q_off, lens, R)
     args, _, hd = _cache8(cache, B, dev, T)
-    L = _lib or lib()
-    cache_p, on = ctypes.byref(args), _stream_on(stream, dev, torch)
+    L, on = _lib or lib(), _stream_on(stream, dev, torch)
     if workspace is None:
         need = c_sz()
-        check(L.f3c_op_cache8_attention_bytes(cache_p, heads, B, offsets, held, int(causal), ctypes.byref(need)))
-        if need.value:
+        check(L.f3c_op_cache8_attention_bytes(args, heads, B, offsets, held, int(causal), need))
+        if need.value and stream is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        elif need.value:
             # (memory of the stream that the call runs on: it is free again once that stream is past the call)
-            with torch.cuda.stream(None if stream is None else torch.cuda.ExternalStream(on)):
+            with torch.cuda.stream(torch.cuda.ExternalStream(on)):
                 workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace: a contiguous tensor on the current GPU expected")
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    check(L.f3c_op_cache8_attention(cache_p, heads, B, offsets, held,
-                                    *_rows("q", q, T[F3C_BF16], R, heads * hd, dev),
-                                    *_rows("o", o, T[F3C_BF16], R, heads * hd, dev), int(causal), int(q_prescaled),
-                                    _ptr(workspace), size, on))
+    ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    bf16 = T[F3C_BF16]
+    check(L.f3c_op_cache8_attention(args, heads, B, offsets, held, *_rows("q", q, bf16, R, heads * hd, dev),
+                                    *_rows("o", o, bf16, R, heads * hd, dev), int(causal), int(q_prescaled), ws, size, on))
 
 
 @functools.lru_cache(maxsize=256)
