@@ -469,7 +469,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // What is read in place of a page that is none: zeros.
 __device__ const u32x4 kNoPage[64] = {};
 
-// Many rows: NW waves of 32 rows each share a page, which goes to LDS by DMA as it
+// Many rows: NW waves of 32 QB rows each share a page, which goes to LDS by DMA as it
 // is, STAGES deep, its 16-byte chunks swizzled by row for conflict-free fragment reads;
 // fragments are widened as they are read. Scores on 32 x 32 instructions, S^T = K Q^T.
 //
@@ -479,9 +479,9 @@ __device__ const u32x4 kNoPage[64] = {};
 // compiler's scheduler behind each group; left alone it gathers the products and then the
 // vector work, and both waves of a SIMD wait for the same unit). Pages at a row's limit, at
 // most a few and the last, go one step after the other, with masks.
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn8Args p) {
-  constexpr int ROWS = 32 * NW, TILE = kPage * HD, STAGES = 5;
+template <int HD, int QB, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
+  constexpr int ROWS = 32 * QB * NW, TILE = kPage * HD, STAGES = 5;
   constexpr int NS = HD / 32, NV = HD / 32;        // pairs of K slices of 16 columns; output tiles of 32
   constexpr int CPR = HD / 16;                     // 16-byte chunks of a row of K
   constexpr int DMA = TILE / 1024;                 // DMA instructions per tile
@@ -495,41 +495,55 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
   const Item it = item_of(p, item);
   const int b = it.b;
   const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
-  const int row_t = it.tile * ROWS, row_w = row_t + wave * 32;
+  const int row_t = it.tile * ROWS, row_w = row_t + wave * 32 * QB;
   // A lane's row: its token and its columns (found anew for the output, not kept)
   auto place = [&](int lane_row, int& tok, int& col) {
     tok = (row_w + lane_row) / p.group;
     col = (head * p.group + row_w + lane_row - tok * p.group) * HD;
   };
-  int tok, qcol;
-  place(r32, tok, qcol);
-  const int lim = tok >= nq ? 0 : p.causal ? max(min(n, n - nq + tok + 1), 0) : n;
+  int lim[QB];
+  bf16x8 qf[QB][2 * NS];
+#pragma unroll
+  for (int j = 0; j < QB; ++j) {
+    int tok, col;
+    place(r32 + 32 * j, tok, col);
+    lim[j] = tok >= nq ? 0 : p.causal ? max(min(n, n - nq + tok + 1), 0) : n;
+    // columns of a lane's fragment 2 i + h: 32 i + 16 g + 8 h on, as a chunk of K holds them
+#pragma unroll
+    for (int s = 0; s < 2 * NS; ++s) {
+      u32x4 raw{0, 0, 0, 0};
+      if (tok < nq)
+        raw = *reinterpret_cast<const u32x4*>(p.q + (q0 + tok) * p.ldq + col + 32 * (s / 2) + 16 * g + 8 * (s % 2));
+      qf[j][s] = __builtin_bit_cast(bf16x8, raw);
+    }
+  }
   // the wave's lowest limit, its highest, the workgroup's highest
   const int lim_lo = p.causal ? n - nq + row_w / p.group + 1 : n;
   const int lim_w = row_w >= nq * p.group ? 0
-                    : p.causal ? max(n - nq + min((row_w + 31) / p.group, nq - 1) + 1, 0) : n;
+                    : p.causal ? max(n - nq + min((row_w + 32 * QB - 1) / p.group, nq - 1) + 1, 0) : n;
   const int lim_hi = p.causal ? max(n - nq + min((row_t + ROWS - 1) / p.group, nq - 1) + 1, 0) : n;
   const int pages = (lim_hi + kPage - 1) / kPage;
   const int begin = min(it.split * p.split_pages, pages), end = min(begin + p.split_pages, pages);
 
-  // Columns of a lane's fragment 2 i + h: 32 i + 16 g + 8 h on, as a chunk of K holds them.
-  bf16x8 qf[2 * NS];
+  // o: outputs; m: the reference that probabilities are relative to, base 2; l: sums of a
+  // lane's own keys. Where masks apply the reference is moved above 2^8 times it; in whole pages
+  // no maximum is taken: a step whose probabilities bring a sum above kMost is taken
+  // back and the reference moved to the maximum or what the sum stands for, the larger.
+  // (Rounding is relative, so a reference far below the maximum costs nothing; sums of 2^24
+  // leave outputs of values up to 2^100 within range.)
+  constexpr float kMost = 0x1p24f;
+  f32x16 o[QB][NV];
+  float m[QB];
+  f32x4 l[QB];
 #pragma unroll
-  for (int s = 0; s < 2 * NS; ++s) {
-    u32x4 raw{0, 0, 0, 0};
-    if (tok < nq)
-      raw = *reinterpret_cast<const u32x4*>(p.q + (q0 + tok) * p.ldq + qcol + 32 * (s / 2) + 16 * g + 8 * (s % 2));
-    qf[s] = __builtin_bit_cast(bf16x8, raw);
+  for (int j = 0; j < QB; ++j) {
+    m[j] = -INFINITY;
+    l[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int t = 0; t < NV; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[j][t][e] = 0.0f;
   }
-  // o: outputs; m: what probabilities are relative to (the largest score, base 2, or up to 2^8
-  // below it), above: the score from which on it moves; l: sums of a lane's own keys.
-  f32x16 o[NV];
-  float m = -INFINITY, above = -INFINITY;
-  f32x4 l{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int t = 0; t < NV; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
   // K: rows of CPR chunks, physical chunk = chunk ^ (row / (16 / CPR)) % CPR, so that 16
   // lanes reading a chunk of 16 rows meet 16 different places of 256 bytes; V: rows of 4.
   auto kswz = [](int row) { return row / (16 / CPR) & (CPR - 1); };
@@ -564,8 +578,8 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     if (at + lane < end) pg = p.c.table[(int64_t)b * p.c.max_pages + at + lane];
     if ((uint32_t)pg >= (uint32_t)p.c.n_pages) pg = -1;
     const int64_t x = (int64_t)(pg < 0 ? 0 : pg) * kvh + head;
-    pks = fp8_scale(p.c.ks[x]);
-    pvs = fp8_scale(p.c.vs[x]);
+    pks = pg < 0 ? 1.0f : fp8_scale(p.c.ks[x]);
+    pvs = pg < 0 ? 1.0f : fp8_scale(p.c.vs[x]);
   };
   auto lane_f = [](float v, int i) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
@@ -582,17 +596,16 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
       asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(blk < DMA ? kdma : vdma), "s"(from), "{m0}"(to) : "memory");
     }
   };
-  // The reference moves to `to`: what was summed up is scaled.
-  auto rescale = [&](float to) __attribute__((always_inline)) {
-    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-    m = to;
-    above = (to + 8.0f) / p.scale;
+  // The reference of block j moves to `to`: what was summed up is scaled.
+  auto rescale = [&](int j, float to) __attribute__((always_inline)) {
+    const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[j] - to);
+    m[j] = to;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) l[e] *= f;
+    for (int e = 0; e < 4; ++e) l[j][e] *= f;
 #pragma unroll
     for (int t = 0; t < NV; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[t][e] *= f;
+      for (int e = 0; e < 16; ++e) o[j][t][e] *= f;
   };
   auto row_sum = [](const bf16x8& f, f32x4 acc) {  // of a lane's own values: 4 x 4 blocks, ones on the left
     const s16x4 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80};
@@ -601,35 +614,51 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(one, u.h[1], acc, 0, 0, 0);
   };
 
+  // Scores of the 32 keys at kat, not interleaved with anything.
+  auto scores = [&](uint32_t kat, float ks, f32x16 (&s)[QB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < NS; ++x) {
+      const u32x4 w = read_k(kat, 0, x);
+      const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
+#pragma unroll
+      for (int j = 0; j < QB; ++j) {
+        s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[j][2 * x], x ? s[j] : zero, 0, 0, 0);
+        s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[j][2 * x + 1], s[j], 0, 0, 0);
+      }
+      fence();
+    }
+  };
   // A page with masks, one step after the other.
   auto masked_page = [&](int i, uint32_t at, float ks, float vs) __attribute__((always_inline)) {
     // (tokens counted from the lane's first; opaque, or the compiler keeps 64 sums over all pages)
-    int there = n - i * kPage - 4 * g, seen = lim - i * kPage - 4 * g;
-    asm("" : "+v"(there), "+v"(seen));
+    int there = n - i * kPage - 4 * g, seen[QB];
+    asm("" : "+v"(there));
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+      seen[j] = lim[j] - i * kPage - 4 * g;
+      asm("" : "+v"(seen[j]));
+    }
 #pragma unroll 1
     for (int h = 0; h < 2; ++h) {
-      f32x16 s;
+      f32x16 s[QB];
+      scores(at + (uint32_t)(h * 32 * HD), ks, s);
+      u32x4 pf[QB][2];
 #pragma unroll
-      for (int x = 0; x < NS; ++x) {
-        const u32x4 w = read_k(at, h, x);
-        const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * x], x ? s : zero, 0, 0, 0);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[2 * x + 1], s, 0, 0, 0);
+      for (int j = 0; j < QB; ++j) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (8 * (e / 4) + e % 4 >= seen[j]) s[j][e] = -INFINITY;
+        const float mx = half_max(max16(s[j])) * p.scale;
+        if (__any(mx > m[j] + 8.0f)) rescale(j, fmaxf(m[j], mx));
+        const float ref = m[j] == -INFINITY ? 0.0f : -m[j];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)
+          pf[j][e / 8][e / 2 % 4] = pack2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[j][e], p.scale, ref)),
+                                          __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][e + 1], p.scale, ref)));
+#pragma unroll
+        for (int u = 0; u < 2; ++u) l[j] = row_sum(__builtin_bit_cast(bf16x8, pf[j][u]), l[j]);
         fence();
       }
-      bf16x8 pf[2];
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (8 * (e / 4) + e % 4 >= seen) s[e] = -INFINITY;
-      const float mx = half_max(max16(s));
-      if (__any(mx > above)) rescale(fmaxf(m, mx * p.scale));
-      const float ref = m == -INFINITY ? 0.0f : -m;
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        pf[e / 8][e % 8] = (bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale, ref));
-#pragma unroll
-      for (int u = 0; u < 2; ++u) l = row_sum(pf[u], l);
-      fence();
 #pragma unroll
       for (int t = 0; t < NV; ++t) {
         u32x2 v[2];
@@ -646,19 +675,23 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
           }
         }
         if (__any(odd)) {
-          f32x16 count = zero;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            bf16x8 sees;
+          for (int j = 0; j < QB; ++j) {
+            f32x16 count = zero;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              sees[e] = (bf16)(16 * u + 8 * (e / 4) + e % 4 < seen ? 1.0f : 0.0f);
-            count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                widen8(nan_bytes(v[0][u]) & 0x38383838u, nan_bytes(v[1][u]) & 0x38383838u, 1.0f), sees, count, 0, 0, 0);
+            for (int u = 0; u < 2; ++u) {
+              bf16x8 sees;
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                sees[e] = (bf16)(16 * u + 8 * (e / 4) + e % 4 < seen[j] ? 1.0f : 0.0f);
+              count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  widen8(nan_bytes(v[0][u]) & 0x38383838u, nan_bytes(v[1][u]) & 0x38383838u, 1.0f), sees, count, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (count[e] > 0.0f) o[j][t][e] = __builtin_nanf("");
+            fence();
           }
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (count[e] > 0.0f) o[t][e] = __builtin_nanf("");
 #pragma unroll
           for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -667,63 +700,78 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const bf16x8 vf = widen8(v[0][u], v[1][u], vs);
-          o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[u], o[t], 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < QB; ++j)
+            o[j][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[j][u]), o[j][t], 0, 0, 0);
         }
         fence();
       }
       there -= 32;
-      seen -= 32;
+#pragma unroll
+      for (int j = 0; j < QB; ++j) seen[j] -= 32;
     }
   };
 
   // Half step: scores `next` of the 32 keys at `kat`, probabilities pc of `cur` (against the
   // reference -ref), the product of pp with the 32 tokens of V at `vat`.
-  auto product_v = [&](uint32_t vat, float vs, const u32x4 (&pp)[2]) __attribute__((always_inline)) {
+  auto product_v = [&](uint32_t vat, float vs, const u32x4 (&pp)[QB][2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < NV; ++t) {
       const u32x2 a = read_v(vat, 0, t, 0), c = read_v(vat, 0, t, 1);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const bf16x8 vf = widen8(a[u], c[u], vs);
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pp[u]), o[t], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < QB; ++j)
+          o[j][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pp[j][u]), o[j][t], 0, 0, 0);
       }
       fence();
     }
   };
-  auto half_step = [&](uint32_t kat, float ks, uint32_t vat, float vs, float ref, const f32x16& cur, f32x16& next,
-                       const u32x4 (&pp)[2], u32x4 (&pc)[2]) __attribute__((always_inline)) {
-    constexpr int G = 4 * NS, N = 16;              // groups of a product, K and V in turn; probabilities
+  auto half_step = [&](uint32_t kat, float ks, uint32_t vat, float vs, const float (&ref)[QB], const f32x16 (&cur)[QB],
+                       f32x16 (&next)[QB], const u32x4 (&pp)[QB][2], u32x4 (&pc)[QB][2]) __attribute__((always_inline)) {
+    // Fragments (K and V in turn), groups of one product each, probabilities. A fragment is
+    // widened a group before its first product, a wave's next product issued only when the
+    // matrix core is about done with the one before (in order, it would hold up what follows).
+    constexpr int F = 4 * NS, G = F * QB, N = 16 * QB;
     u32x4 kr[2];                                   // raw fragments of K (a pair of slices each)
     u32x2 vr[2][2];                                // and of V (an output tile each)
+    bf16x8 frag[2];
     float ex[N];
+    auto widen = [&](auto xc) {
+      constexpr int x = decltype(xc)::value, a = x / 2;
+      if constexpr (x % 2 == 0) frag[0] = widen8(kr[a / 2 % 2][2 * (a % 2)], kr[a / 2 % 2][2 * (a % 2) + 1], ks);
+      else frag[1] = widen8(vr[a / 2 % 2][0][a % 2], vr[a / 2 % 2][1][a % 2], vs);
+    };
     kr[0] = read_k(kat, 0, 0);
     vr[0][0] = read_v(vat, 0, 0, 0);
     vr[0][1] = read_v(vat, 0, 0, 1);
+    widen(std::integral_constant<int, 0>{});
+    fence();
     static_for<G>([&](auto nc) {
-      constexpr int x = decltype(nc)::value, a = x / 2;
-      if constexpr (x % 4 == 0 && x + 4 < G) {
+      constexpr int y = decltype(nc)::value, x = y / QB, j = y % QB, a = x / 2;
+      if constexpr (j == 0 && x % 4 == 0 && x + 4 < F) {
         kr[(a / 2 + 1) % 2] = read_k(kat, 0, a / 2 + 1);
         vr[(a / 2 + 1) % 2][0] = read_v(vat, 0, a / 2 + 1, 0);
         vr[(a / 2 + 1) % 2][1] = read_v(vat, 0, a / 2 + 1, 1);
       }
-      if constexpr (x % 2 == 0) {
-        const bf16x8 kf = widen8(kr[a / 2 % 2][2 * (a % 2)], kr[a / 2 % 2][2 * (a % 2) + 1], ks);
-        next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[a], a ? next : zero, 0, 0, 0);
-      } else {
-        const bf16x8 vf = widen8(vr[a / 2 % 2][0][a % 2], vr[a / 2 % 2][1][a % 2], vs);
-        o[a / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pp[a % 2]), o[a / 2], 0, 0, 0);
-      }
+      if constexpr (x % 2 == 0)
+        next[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[0], qf[j][a], a ? next[j] : zero, 0, 0, 0);
+      else
+        o[j][a / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[1], __builtin_bit_cast(bf16x8, pp[j][a % 2]), o[j][a / 2],
+                                                              0, 0, 0);
       // exponentials, converted a group later
-      constexpr int E0 = x * N / G, E1 = (x + 1) * N / G, C0 = x ? (x - 1) * N / G & ~1 : 0,
-                    C1 = x + 1 == G ? N : E0 & ~1;
+      constexpr int E0 = y * N / G, E1 = (y + 1) * N / G, C0 = y ? (y - 1) * N / G & ~1 : 0,
+                    C1 = y + 1 == G ? N : E0 & ~1;
       static_for<E1 - E0>([&](auto k) {
         constexpr int i = E0 + decltype(k)::value;
-        ex[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[i], p.scale, ref));
+        ex[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[i / 16][i % 16], p.scale, ref[i / 16]));
       });
+      if constexpr (j == QB - 1 && x + 1 < F) widen(std::integral_constant<int, x + 1>{});
       static_for<(C1 - C0) / 2>([&](auto k) {
         constexpr int i = C0 + 2 * decltype(k)::value;
-        pc[i / 8][i / 2 % 4] = pack2(ex[i], ex[i + 1]);
-        if constexpr (i % 8 == 6) l = row_sum(__builtin_bit_cast(bf16x8, pc[i / 8]), l);
+        pc[i / 16][i / 8 % 2][i / 2 % 4] = pack2(ex[i], ex[i + 1]);
+        if constexpr (i % 8 == 6) l[i / 16] = row_sum(__builtin_bit_cast(bf16x8, pc[i / 16][i / 8 % 2]), l[i / 16]);
       });
       fence();
     });
@@ -740,7 +788,9 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     __builtin_amdgcn_s_barrier();                  // the first page has landed
     fence();
     int stage = 0;                                 // of page i
+    int synced = -1;                               // the last page that the next was called for
     auto sync = [&](int i) {                       // page i + 1 has landed, the stage of i - 2 is free
+      synced = i;
       wait_vm<(STAGES - 4) * DQ>();
       __builtin_amdgcn_s_barrier();
       fence();
@@ -749,55 +799,63 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     auto none = [&](int i) { return __builtin_amdgcn_readlane(pg, i - base) < 0; };
     auto at_stage = [&](int s) { return (uint32_t)(s * 2 * TILE); };
     auto after = [&](int s) { return s == STAGES - 1 ? 0 : s + 1; };
-    // Pages that all of the wave's rows see, in half steps. A segment of them ends where a score
-    // calls for a move of the reference (a branch within the loop would copy the outputs
-    // at every step): it starts with scores of its own and no probabilities before them.
+    // Pages that all of the wave's rows see, in half steps. A segment of them ends where the
+    // reference has to move (a branch within the loop would copy the outputs at every step):
+    // it starts with scores of its own and no probabilities before them.
     const int whole = row_w >= nq * p.group ? first : min(max(lim_lo / kPage, first), last);
     int t = 2 * first;
     while (t < 2 * whole) {
-      f32x16 s0, s1;
-      u32x4 p0[2], p1[2];                          // (pairs, as bf16)
-      p1[0] = p1[1] = u32x4{0, 0, 0, 0};
+      f32x16 s0[QB], s1[QB];
+      u32x4 p0[QB][2], p1[QB][2];                  // (pairs, as bf16)
+#pragma unroll
+      for (int j = 0; j < QB; ++j) p1[j][0] = p1[j][1] = u32x4{0, 0, 0, 0};
       int i = t / 2;
       uint32_t vat = at_stage(stage) + (uint32_t)(8 * (t % 2));      // (zeros times V of this page, which every row sees)
       float vsb = lane_f(pvs, i - base);
-      {
-        const uint32_t kat = at_stage(stage) + (uint32_t)(32 * HD * (t % 2));
-        const float ks = lane_f(pks, i - base);
+      scores(at_stage(stage) + (uint32_t)(32 * HD * (t % 2)), lane_f(pks, i - base), s0);
 #pragma unroll
-        for (int x = 0; x < NS; ++x) {
-          const u32x4 w = read_k(kat, 0, x);
-          const bf16x8 a = widen8(w[0], w[1], ks), c = widen8(w[2], w[3], ks);
-          s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[2 * x], x ? s0 : zero, 0, 0, 0);
-          s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c, qf[2 * x + 1], s0, 0, 0, 0);
-          fence();
-        }
-        const float mx = half_max(max16(s0));
-        if (!none(i) && __any(mx > above)) rescale(fmaxf(m, mx * p.scale));
+      for (int j = 0; j < QB; ++j) {
+        const float mx = half_max(max16(s0[j])) * p.scale, sum = half_sum(l[j][0]);
+        if (!none(i) && __any(mx > m[j] + 8.0f || sum > 0x1p12f))
+          rescale(j, fmaxf(fmaxf(m[j], mx), m[j] + __builtin_amdgcn_logf(sum)));
       }
       // A half step at t, then whether the segment ends. Where it has ended already (behind the
       // first of a pair: the loop has one exit, or the outputs would be copied at it), it is
       // no step: the product with pp and no probabilities.
       bool done = false;
-      auto step = [&](const f32x16& cur, f32x16& next, const u32x4 (&pp)[2], u32x4 (&pc)[2])
+      auto step = [&](const f32x16 (&cur)[QB], f32x16 (&next)[QB], const u32x4 (&pp)[QB][2], u32x4 (&pc)[QB][2])
                       __attribute__((always_inline)) {
         const bool second = t % 2;
-        if (!done && !second) sync(i);
+        if (!done && !second && synced != i) sync(i);
         // (behind the last half step scores of this page again: the next one may hold NaN that not
         // all rows see, which no step may take)
         const bool next_page = second && t + 1 < 2 * whole;
         const int nx = next_page ? i + 1 : i;
         const uint32_t here = at_stage(stage), kat = next_page ? at_stage(after(stage)) : here + 32 * HD;
         // (a page that is none: its scores are 0 and its probabilities 0)
-        half_step(kat, lane_f(pks, nx - base), vat, vsb, done || none(i) ? -INFINITY : -m, cur, next, pp, pc);
-        if (!done) {
+        float ref[QB], before[QB];
+#pragma unroll
+        for (int j = 0; j < QB; ++j) {
+          ref[j] = done || none(i) ? -INFINITY : -m[j];
+          before[j] = l[j][0];
+        }
+        half_step(kat, lane_f(pks, nx - base), vat, vsb, ref, cur, next, pp, pc);
+        bool much = false;
+#pragma unroll
+        for (int j = 0; j < QB; ++j) much = much || l[j][0] > kMost;
+        if (__any(much)) {                         // rare; the step is taken again in the next segment
+#pragma unroll
+          for (int j = 0; j < QB; ++j) {
+            l[j][0] = before[j];
+            pc[j][0] = pc[j][1] = u32x4{0, 0, 0, 0};
+          }
+          done = true;
+        } else if (!done) {
           vat = here + (uint32_t)(8 * (t % 2));
           vsb = lane_f(pvs, i - base);
-          done = t + 1 == 2 * whole;
           if (second) ++i, stage = after(stage);
-          ++t;
+          done = ++t == 2 * whole;
         }
-        done = done || (!none(i) && __any(half_max(max16(next)) > above));
       };
       do {
         step(s0, s1, p1, p0);
@@ -813,35 +871,38 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_rows(Attn
     }
   }
   wait_vm<0>();                                    // no DMA into LDS that another workgroup may get
-  const float sum = half_sum(l[0]);
-  int again = r32;
-  asm("" : "+v"(again));
-  place(again, tok, qcol);
-  if (it.splits > 1) {
-    if (tok >= nq) return;
-    const int64_t slot = ((int64_t)item * kvh + head) * ROWS + wave * 32 + r32;
 #pragma unroll
-    for (int t = 0; t < NV; ++t)
+  for (int j = 0; j < QB; ++j) {
+    const float sum = half_sum(l[j][0]);
+    int again = r32 + 32 * j, tok, col;
+    asm("" : "+v"(again));
+    place(again, tok, col);
+    if (tok >= nq) continue;
+    if (it.splits > 1) {
+      const int64_t slot = ((int64_t)item * kvh + head) * ROWS + wave * 32 * QB + again;
 #pragma unroll
-      for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<f32x4*>(p.part_o + slot * HD + 32 * t + 2 * e + 4 * g) =
-            f32x4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]};
-    if (g == 0) {
-      p.part_ml[2 * slot] = m;
-      p.part_ml[2 * slot + 1] = sum;
-    }
-  } else if (tok < nq) {
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    bf16* out = p.o + (q0 + tok) * p.ldo + qcol;
+      for (int t = 0; t < NV; ++t)
 #pragma unroll
-    for (int t = 0; t < NV; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; e += 4) {
-        bf16x4 w;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) w[x] = (bf16)(o[t][e + x] * inv);
-        *reinterpret_cast<bf16x4*>(out + 32 * t + 2 * e + 4 * g) = w;
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<f32x4*>(p.part_o + slot * HD + 32 * t + 2 * e + 4 * g) =
+              f32x4{o[j][t][e], o[j][t][e + 1], o[j][t][e + 2], o[j][t][e + 3]};
+      if (g == 0) {
+        p.part_ml[2 * slot] = m[j];
+        p.part_ml[2 * slot + 1] = sum;
       }
+    } else {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      bf16* out = p.o + (q0 + tok) * p.ldo + col;
+#pragma unroll
+      for (int t = 0; t < NV; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          bf16x4 w;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) w[x] = (bf16)(o[j][t][e + x] * inv);
+          *reinterpret_cast<bf16x4*>(out + 32 * t + 2 * e + 4 * g) = w;
+        }
+    }
   }
 }
 
@@ -893,7 +954,7 @@ Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, size_t 
   const int group = heads / c.kv_heads;
   int64_t most = 0;
   for (int b = 0; b < rows.B; ++b) most = std::max(most, (int64_t)(rows.off[b + 1] - rows.off[b]) * group);
-  r.rows = most <= 16 ? 16 : 128;
+  r.rows = most <= 16 ? 16 : c.hd < 128 && !getenv("C8_QB1") ? 256 : 128;
   r.tiles.B = r.items.B = rows.B;
   int64_t work = 0;                                // pages of all tiles and heads
   int longest = 0;
@@ -924,7 +985,9 @@ template <int HD>
 hipError_t launch_attn8(const Attn8Args& a, const Plan& pl, hipStream_t s) {
   const int64_t items = (int64_t)a.items.off[a.items.B] * a.c.kv_heads;
   if (!items) return hipSuccess;
-  if (pl.rows == 128) launch((k_cache8_rows<HD, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
+  if (pl.rows == 256) {
+    if constexpr (HD < 128) launch((k_cache8_rows<HD, 2, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
+  } else if (pl.rows == 128) launch((k_cache8_rows<HD, 1, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
   else if (items <= 256) launch((k_cache8_attn<HD, 8>), dim3((uint32_t)items), dim3(512), 0, s, a);
   else launch((k_cache8_attn<HD, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
   if (pl.split) {
