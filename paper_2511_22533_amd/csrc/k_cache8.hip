@@ -1,6 +1,6 @@
 // The cache of 8-bit keys and values (cache8.h): appending to it, and attention over it.
 #include <algorithm>
-#include <cstdlib>
+#include <cmath>
 #include <type_traits>
 #include <utility>
 
@@ -139,8 +139,12 @@ __global__ __launch_bounds__(2 * HD) void k_cache8_append(AppendArgs p) {
 struct Attn8Args {
   Cache8 c;
   Lens len;
-  Segs rows, tiles, items;                         // tiles: of `tile_rows` rows (token, head of the group); items: tiles
-                                                   // times the splits of their sample's pages; both counted through
+  Segs rows;
+  // Samples by falling length: the y-th longest is order[y], its row tiles (of tile_rows rows: token,
+  // head of the group) are tiles.off[y].., its items (tiles times splits of its pages)
+  // items.off[y]..
+  Segs tiles, items;
+  uint8_t order[kMaxBatch];
   const bf16* q;
   bf16* o;
   int64_t ldq, ldo;
@@ -150,19 +154,23 @@ struct Attn8Args {
   float* part_ml;                                  // and [..][tile_rows][2]: reference max, sum
 };
 
-// A workgroup's sample, tile (of the sample) and pages [begin, end) of those below lim (the
-// highest limit of a tile's rows). One split: the output is the kernel's own.
+// A workgroup's work. Workgroups go round the XCDs in turn: heads are fastest, so that an XCD
+// (with its L2) sees few of them, and the longest items come first (later rows' under a
+// causal mask, and longer samples').
 struct Item {
-  int b, tile, splits, split;
+  int item, head, b, tile, splits, split;
 };
-__device__ __forceinline__ Item item_of(const Attn8Args& p, int item) {
+__device__ __forceinline__ Item item_of(const Attn8Args& p) {
   Item r;
-  r.b = find_segment_wave(p.items.off, p.items.B, item);
-  const int tiles = p.tiles.off[r.b + 1] - p.tiles.off[r.b];
-  r.splits = (p.items.off[r.b + 1] - p.items.off[r.b]) / tiles;
-  const int local = item - p.items.off[r.b];
-  r.tile = local / r.splits;
-  r.split = local - r.tile * r.splits;
+  r.item = blockIdx.x / p.c.kv_heads;
+  r.head = blockIdx.x - r.item * p.c.kv_heads;
+  const int y = find_segment_wave(p.items.off, p.items.B, r.item);
+  r.b = p.order[y];
+  const int tiles = p.tiles.off[y + 1] - p.tiles.off[y], local = r.item - p.items.off[y];
+  r.splits = (p.items.off[y + 1] - p.items.off[y]) / tiles;
+  const int back = local / r.splits;
+  r.tile = tiles - 1 - back;
+  r.split = local - back * r.splits;
   return r;
 }
 
@@ -209,10 +217,8 @@ __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_attn(Attn
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane >> 4, r16 = lane & 15;
-  const int kvh = p.c.kv_heads, logical = xcd_logical_id(blockIdx.x, p.items.off[p.items.B] * kvh);
-  const int item = logical / kvh, head = logical - item * kvh;
-  const Item it = item_of(p, item);
-  const int b = it.b;
+  const Item it = item_of(p);
+  const int kvh = p.c.kv_heads, b = it.b, head = it.head, item = it.item;
   const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
   const int row = it.tile * 16 + r16, tok = row / p.group;
   const bool in = tok < nq;
@@ -490,10 +496,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
   __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * TILE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = lane >> 5, r32 = lane & 31;
-  const int n_items = p.items.off[p.items.B], kvh = p.c.kv_heads, logical = xcd_logical_id(blockIdx.x, n_items * kvh);
-  const int head = logical / n_items, item = n_items - 1 - logical % n_items;        // (causal: the longest first)
-  const Item it = item_of(p, item);
-  const int b = it.b;
+  const Item it = item_of(p);
+  const int kvh = p.c.kv_heads, b = it.b, head = it.head, item = it.item;
   const int q0 = p.rows.off[b], nq = p.rows.off[b + 1] - q0, n = p.len.n[b];
   const int row_t = it.tile * ROWS, row_w = row_t + wave * 32 * QB;
   // A lane's row: its token and its columns (found anew for the output, not kept)
@@ -913,12 +917,12 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p) {
   const int kvh = p.c.kv_heads, x = blockIdx.x * 256 + threadIdx.x, d = x % (HD / 4) * 4, y = x / (HD / 4);
   const int r = y % p.tile_rows, z = __builtin_amdgcn_readfirstlane(y / p.tile_rows), head = z % kvh, tile = z / kvh;
   if (tile >= p.tiles.off[p.tiles.B]) return;
-  const int b = find_segment_wave(p.tiles.off, p.tiles.B, tile), q0 = p.rows.off[b];
-  const int splits = (p.items.off[b + 1] - p.items.off[b]) / (p.tiles.off[b + 1] - p.tiles.off[b]);
-  const int row = (tile - p.tiles.off[b]) * p.tile_rows + r, t = row / p.group;
+  const int s0 = find_segment_wave(p.tiles.off, p.tiles.B, tile), b = p.order[s0], q0 = p.rows.off[b];
+  const int tiles = p.tiles.off[s0 + 1] - p.tiles.off[s0], splits = (p.items.off[s0 + 1] - p.items.off[s0]) / tiles;
+  const int back = tile - p.tiles.off[s0], row = (tiles - 1 - back) * p.tile_rows + r, t = row / p.group;
   if (splits < 2 || t >= p.rows.off[b + 1] - q0) return;
   const int64_t step = (int64_t)kvh * p.tile_rows;
-  const int64_t slot = ((int64_t)(p.items.off[b] + (tile - p.tiles.off[b]) * splits) * kvh + head) * p.tile_rows + r;
+  const int64_t slot = ((int64_t)(p.items.off[s0] + back * splits) * kvh + head) * p.tile_rows + r;
   float top = -INFINITY;
   for (int s = 0; s < splits; ++s) top = fmaxf(top, p.part_ml[2 * (slot + s * step)]);
   float sum = 0.0f;
@@ -942,6 +946,7 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p) {
 // How a call is cut: row tiles, and splits of the pages of their sample.
 struct Plan {
   Segs tiles, items;
+  uint8_t order[kMaxBatch];
   int rows, split_pages;                           // rows: of a tile
   bool split;                                      // some sample's pages are split
   size_t bytes(const Cache8& c) const {
@@ -949,36 +954,84 @@ struct Plan {
   }
 };
 
-Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, size_t ws_bytes) {
-  Plan r{};
-  const int group = heads / c.kv_heads;
-  int64_t most = 0;
-  for (int b = 0; b < rows.B; ++b) most = std::max(most, (int64_t)(rows.off[b + 1] - rows.off[b]) * group);
-  r.rows = most <= 16 ? 16 : c.hd < 128 && !getenv("C8_QB1") ? 256 : 128;
-  r.tiles.B = r.items.B = rows.B;
-  int64_t work = 0;                                // pages of all tiles and heads
-  int longest = 0;
+// What a form of the kernel takes, in us on MI355X: a page of one workgroup's rows while a CU has
+// one of them (first) or more (page, each), and what a workgroup costs beside its pages (own).
+// Of 16 rows, page is a CU's throughput and first the time from page to page of one wave.
+// Measured: 32, 64 and 128 columns, 16 heads, 2048 to 32768 queries over 16384 keys and 32 to 32768
+// over 1374; the pick is within 10% of the best of the forms and splits measured there.
+struct FormCost {
+  int rows, hd;
+  double first, page, own;
+};
+constexpr FormCost kForms[] = {
+    {16, 32, 1.0, 0.09, 0.3},  {16, 64, 1.3, 0.14, 0.3},   {16, 128, 3.0, 0.37, 0.4},  {128, 32, 0.7, 0.42, 1.6},
+    {128, 64, 0.95, 0.6, 1.6}, {128, 128, 1.16, 1.1, 3.0}, {256, 32, 0.94, 0.9, 3.0},  {256, 64, 1.25, 1.13, 3.0},
+};
+constexpr double kLaunchUs = 5.0, kJoinUs = 5.0, kPartialBytesPerUs = 4e6, kReadBytesPerUs = 5e6;
+constexpr int kLeastSplit = 8;                     // pages
+
+Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool causal, size_t ws_bytes) {
+  Plan best{};
+  const int group = heads / c.kv_heads, B = rows.B;
   int pages[kMaxBatch];
-  for (int b = 0; b < rows.B; ++b) {
-    const int64_t n = (int64_t)(rows.off[b + 1] - rows.off[b]) * group, tiles = (n + r.rows - 1) / r.rows;
+  int64_t most_rows = 0;
+  for (int b = 0; b < B; ++b) {
     pages[b] = (len.n[b] + kPage - 1) / kPage;
-    r.tiles.off[b + 1] = r.tiles.off[b] + (int)tiles;
-    work += tiles * pages[b] * c.kv_heads;
-    if (tiles) longest = std::max(longest, pages[b]);
+    best.order[b] = (uint8_t)b;
+    most_rows = std::max(most_rows, (int64_t)(rows.off[b + 1] - rows.off[b]) * group);
   }
-  const char* e1 = getenv("C8_SMALL"); const char* e2 = getenv("C8_ROWS");
-  const int64_t want = r.rows == 16 ? (e1 ? atoi(e1) : 1024) : (e2 ? atoi(e2) : 512), least = r.rows == 16 ? 16 : 8;
-  r.split_pages = (int)std::max<int64_t>(std::max<int64_t>(least, (work + want - 1) / want), 1);
-  if ((int64_t)r.tiles.off[rows.B] * c.kv_heads >= want) r.split_pages = std::max(r.split_pages, longest);
-  for (;; r.split_pages *= 2) {
-    r.split = false;
-    for (int b = 0; b < rows.B; ++b) {
-      const int splits = std::max(1, (pages[b] + r.split_pages - 1) / r.split_pages);
-      r.items.off[b + 1] = r.items.off[b] + (r.tiles.off[b + 1] - r.tiles.off[b]) * splits;
-      r.split = r.split || (splits > 1 && r.tiles.off[b + 1] > r.tiles.off[b]);
+  std::stable_sort(best.order, best.order + B, [&](int x, int y) { return pages[x] > pages[y]; });
+  int longest = 1;
+  for (int y = B - 1; y >= 0; --y)
+    if (rows.off[best.order[y] + 1] > rows.off[best.order[y]]) longest = std::max(pages[best.order[y]], 1);
+  double best_t = 0.0;
+  for (const FormCost& f : kForms) {
+    if (f.hd != c.hd || (f.rows > 16 && most_rows <= 16)) continue;
+    int tiles[kMaxBatch];
+    double work = 0.0, read = 0.0;                 // pages of all tiles and heads; bytes
+    for (int y = 0; y < B; ++y) {
+      const int b = best.order[y], nq = rows.off[b + 1] - rows.off[b];
+      tiles[y] = (int)(((int64_t)nq * group + f.rows - 1) / f.rows);
+      const double seen = pages[b] - (causal ? std::min(nq, len.n[b]) / (2.0 * kPage) : 0.0);
+      work += tiles[y] * std::max(seen, 0.5) * c.kv_heads;
+      if (tiles[y]) read += 2.0 * pages[b] * kPage * c.hd * c.kv_heads;
     }
-    if (r.bytes(c) <= ws_bytes) return r;
+    for (int k = 1; k <= 128; k = k < 4 ? k + 1 : k * 2) {
+      const int p = (longest + k - 1) / k;
+      if (k > 1 && p < kLeastSplit) break;
+      int64_t all = 0;
+      for (int y = 0; y < B; ++y) all += (int64_t)tiles[y] * std::max(1, (pages[best.order[y]] + p - 1) / p);
+      const double items = (double)all * c.kv_heads, need = k < 2 ? 0.0 : items * f.rows * (c.hd + 2) * 4.0;
+      if (k > 1 && (need > (double)ws_bytes || items >= (1 << 23))) break;
+      const double per_cu = items / 256.0, load = work / 256.0;
+      double t;
+      if (f.rows == 16) {
+        t = std::max({load * f.page + per_cu * f.own, p * f.first / (items <= 256.0 ? 8.0 : 4.0), read / kReadBytesPerUs});
+      } else if (per_cu <= 1.0) {
+        t = p * f.first + f.own;
+      } else {
+        // whole rounds, or pieces of different length, the longest first
+        const double uneven = causal ? 0.35 * p : (std::ceil(per_cu) / per_cu - 1.0) * 0.5 * load;
+        t = std::max(p * f.first, (load + uneven) * f.page) + per_cu * f.own;
+      }
+      t += kLaunchUs + (k > 1 ? kJoinUs + 2.0 * need / kPartialBytesPerUs : 0.0);
+      if (best_t == 0.0 || t < best_t) {
+        best_t = t;
+        best.rows = f.rows;
+        best.split_pages = p;
+      }
+    }
   }
+  best.tiles.B = best.items.B = B;
+  for (int y = 0; y < B; ++y) {
+    const int b = best.order[y];
+    const int n = (int)(((int64_t)(rows.off[b + 1] - rows.off[b]) * group + best.rows - 1) / best.rows);
+    const int splits = std::max(1, (pages[b] + best.split_pages - 1) / best.split_pages);
+    best.tiles.off[y + 1] = best.tiles.off[y] + n;
+    best.items.off[y + 1] = best.items.off[y] + n * splits;
+    best.split = best.split || (splits > 1 && n);
+  }
+  return best;
 }
 
 template <int HD>
@@ -1024,18 +1077,19 @@ hipError_t launch_cache8_append(const Cache8& c, int dt, const Lens& len, const 
 }
 
 size_t cache8_attention_bytes(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool causal) {
-  return plan(c, heads, rows, len, ~(size_t)0).bytes(c);
+  return plan(c, heads, rows, len, causal, ~(size_t)0).bytes(c);
 }
 
 hipError_t launch_cache8_attention(const Cache8& c, int heads, const Segs& rows, const Lens& len, const void* q,
                                    int64_t ldq, void* o, int64_t ldo, bool causal, bool q_scaled, void* ws,
                                    size_t ws_bytes, hipStream_t s) {
   const Lens held = c.n_pages ? len : Lens{};      // no pages: no tokens
-  const Plan pl = plan(c, heads, rows, held, ws_bytes);
+  const Plan pl = plan(c, heads, rows, held, causal, ws_bytes);
   const int64_t slots = (int64_t)pl.items.off[rows.B] * c.kv_heads * pl.rows;
-  Attn8Args a{c, held, rows, pl.tiles, pl.items, (const bf16*)q, (bf16*)o, ldq, ldo, heads / c.kv_heads, causal,
+  Attn8Args a{c, held, rows, pl.tiles, pl.items, {}, (const bf16*)q, (bf16*)o, ldq, ldo, heads / c.kv_heads, causal,
               pl.rows, pl.split_pages, q_scaled ? 1.0f : attention_q_scale(c.hd), (float*)ws,
               (float*)ws + slots * c.hd};
+  std::copy(pl.order, pl.order + rows.B, a.order);
   switch (c.hd) {
     case 32: return launch_attn8<32>(a, pl, s);
     case 64: return launch_attn8<64>(a, pl, s);
