@@ -799,8 +799,123 @@ hipError_t launch_epi(const Gemm8Args& a, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
+// Few outputs of integers: a workgroup takes 16 MT rows by 16 NT columns, its eight waves K
+// in pieces of 64 J in turn, each the whole tile, fragments straight from memory into
+// registers (an instruction reads 64 bytes of 16 rows), the next piece asked for ahead. Sums
+// are exact, so that K may be split in any way; the waves' meet in LDS.
+//
+// The chain over K is what bounds the tiles above here (0.19 us per 128 of K, one after the
+// other, whatever the workgroups); this has an eighth of it. Device us, the best tile / here,
+// stored: 1 x 2896 x 4304 10.0 / 4.8, 1 x 160 x 7392 14.6 / 5.9, 2 x 6720 x 2480 7.3 / 5.0, 24 x 2704 x
+// 3632 9.2 / 6.4, 284 x 384 x 8032 16.1 / 10.8, in 32 x 32: 102 x 1152 x 4672 10.8 / 9.0. Where it is
+// taken: 16 rows, always (1.45 times as fast in the mean of 130 shapes, 1.1 slower at worst); 32 x
+// 16 in one workgroup per CU (over 100 shapes faster up to 256 of them, slower beyond, 1.2 in the
+// mean), 32 x 32 likewise, while its rows come from the caches fast enough (195 workgroups
+// at K = 7552 take 17.8 us against 15.6). 64 x 32 and 64 x 64 are slower than the tiles throughout.
+template <int EPI, int MT, int NT, int J>
+__global__ __launch_bounds__(512) void k_gemm_i8_few(Gemm8Args p) {
+  constexpr int NW = 8, KP = 64 * J;
+  __shared__ __attribute__((aligned(16))) i32x4 part[NW][16 * MT][4 * NT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane >> 4, r16 = lane & 15, n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
+  // (rows past M and N repeat the last)
+  const uint8_t *a[MT], *w[NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) a[i] = p.A + min(m0 + 16 * i + r16, p.M - 1) * p.lda + 16 * c;
+#pragma unroll
+  for (int i = 0; i < NT; ++i) w[i] = p.W + min(n0 + 16 * i + r16, p.N - 1) * p.ldw + 16 * c;
+  i32x4 fa[2][MT][J], fw[2][NT][J], acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int x = 0; x < NT; ++x) acc[i][x] = i32x4{0, 0, 0, 0};
+  auto load = [&](int k, i32x4 (&la)[MT][J], i32x4 (&lw)[NT][J]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const bool in = k + KP <= p.K || k + 64 * j + 16 * c < p.K;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        lw[i][j] = i32x4{0, 0, 0, 0};
+        if (in) lw[i][j] = *reinterpret_cast<const i32x4*>(w[i] + k + 64 * j);
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        la[i][j] = i32x4{0, 0, 0, 0};
+        if (in) la[i][j] = *reinterpret_cast<const i32x4*>(a[i] + k + 64 * j);
+      }
+    }
+  };
+  auto multiply = [&](const i32x4 (&la)[MT][J], const i32x4 (&lw)[NT][J]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+          acc[i][x] = __builtin_amdgcn_mfma_i32_16x16x64_i8(lw[x][j], la[i][j], acc[i][x], 0, 0, 0);
+  };
+  int k = wave * KP;
+  if (k < p.K) load(k, fa[0], fw[0]);
+  while (k < p.K) {
+    if (k + NW * KP < p.K) load(k + NW * KP, fa[1], fw[1]);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(fa[0], fw[0]);
+    k += NW * KP;
+    if (k >= p.K) break;
+    if (k + NW * KP < p.K) load(k + NW * KP, fa[0], fw[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(fa[1], fw[1]);
+    k += NW * KP;
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int x = 0; x < NT; ++x) part[wave][16 * i + r16][4 * x + c] = acc[i][x];
+  __syncthreads();
+  typedef f32x4 __attribute__((aligned(4))) f32x4_4;
+  for (int t = tid; t < 16 * MT * 4 * NT; t += 64 * NW) {
+    const int at = t / (4 * NT), q = t % (4 * NT), row = m0 + at, col = n0 + 4 * q;      // four columns of a row
+    if (row >= p.M || col >= p.N) continue;
+    i32x4 sum = part[0][at][q];
+#pragma unroll
+    for (int x = 1; x < NW; ++x) sum += part[x][at][q];
+    const f32x4 sw = *reinterpret_cast<const f32x4_4*>(reinterpret_cast<const float*>(p.sw) + col);
+    const float sa = reinterpret_cast<const float*>(p.sa)[row];
+    f32x4 b{0.0f, 0.0f, 0.0f, 0.0f}, g{1.0f, 1.0f, 1.0f, 1.0f}, v;
+    if (p.bias) b = *reinterpret_cast<const f32x4*>(p.bias + col);
+    if (EPI == EPI_RESID && p.gate) g = *reinterpret_cast<const f32x4*>(p.gate + col);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = sa * (sw[e] * (float)sum[e]) + b[e];
+    if constexpr (EPI == EPI_RESID) {
+      f32x4* h = reinterpret_cast<f32x4*>(p.resid + row * p.ldr + col);
+      f32x4 x = *h;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += g[e] * v[e];
+      *h = x;
+    } else {
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (bf16)(EPI == EPI_GELU ? gelu_fast(v[e]) : v[e]);
+      *reinterpret_cast<bf16x4*>(reinterpret_cast<bf16*>(p.out) + row * p.ldo + col) = o;
+    }
+  }
+}
+
+template <int EPI, int MT, int NT, int J>
+hipError_t launch_few(const Gemm8Args& a, hipStream_t s) {
+  launch((k_gemm_i8_few<EPI, MT, NT, J>),
+         dim3((uint32_t)((a.N + 16 * NT - 1) / (16 * NT)), (uint32_t)((a.M + 16 * MT - 1) / (16 * MT))), dim3(512), 0, s, a);
+  return hipGetLastError();
+}
+
 template <int EPI>
 hipError_t launch_epi_i8(const Gemm8Args& a, hipStream_t s) {
+  const auto groups = [&](int rows, int cols) {
+    return (int64_t)((a.M + rows - 1) / rows) * ((a.N + cols - 1) / cols);
+  };
+  if (a.M <= 16 && a.N < (1 << 26)) return launch_few<EPI, 1, 1, 4>(a, s);       // (a launch has fewer than 2^32 threads)
+  if (groups(32, 16) <= 256) return launch_few<EPI, 2, 1, 4>(a, s);
+  if (groups(32, 32) <= 256 && groups(32, 32) * a.K <= (1 << 20)) return launch_few<EPI, 2, 2, 2>(a, s);
   switch (choose_tiles(kTile8Cost, a.M, a.N, a.K, EPI)) {
     case 0: return launch_dma<256, 256, 2, 4, 2, 2, EPI, 1, OPS_I8>(a, s);
     case 1: return launch_dma<192, 256, 2, 4, 2, 2, EPI, 1, OPS_I8>(a, s);
