@@ -534,7 +534,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
   // no maximum is taken: a step whose probabilities bring a sum above kMost is taken
   // back and the reference moved to the maximum or what the sum stands for, the larger.
   // (Rounding is relative, so a reference far below the maximum costs nothing; sums of 2^24
-  // leave outputs of values up to 2^100 within range.)
+  // leave outputs of values up to 2^100 within range. What is below 2^-102 of a row's largest
+  // probability may count as none: exponentials end at 2^-126.)
   constexpr float kMost = 0x1p24f;
   f32x16 o[QB][NV];
   float m[QB];
@@ -1002,7 +1003,8 @@ Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool ca
       int64_t all = 0;
       for (int y = 0; y < B; ++y) all += (int64_t)tiles[y] * std::max(1, (pages[best.order[y]] + p - 1) / p);
       const double items = (double)all * c.kv_heads, need = k < 2 ? 0.0 : items * f.rows * (c.hd + 2) * 4.0;
-      if (k > 1 && (need > (double)ws_bytes || items >= (1 << 23))) break;
+      // (a launch has fewer than 2^32 threads; the join's count is 32 bits and signed)
+      if (k > 1 && (need > (double)ws_bytes || items >= (1 << 23) || items * f.rows * (c.hd / 4) >= 2147483648.0)) break;
       const double per_cu = items / 256.0, load = work / 256.0;
       double t;
       if (f.rows == 16) {

@@ -324,6 +324,124 @@ def test_attention_far_pages(torch, f3c):
         assert np.array_equal(t[pages - a.shape[0]:].cpu().numpy(), a)
 
 
+# ----------------------------------------------------------------------------------- attention of many rows, on the GPU
+
+def _random_pool(torch, f3c, gen, lens, heads, hd):
+    """Random codes with scales of 1/2 to 4, NaN behind each sample's last token, pages without order, and the slots."""
+    table, pages = _table(np.random.default_rng(len(lens)), lens)
+    slots = torch.from_numpy(cache8.SLOTS).cuda()
+    code = lambda: torch.randn(pages, heads, 64, hd, generator=gen, device="cuda").to(torch.float8_e4m3fn).view(torch.uint8)  # noqa: E731
+    scale = lambda: torch.randint(126, 130, (pages, heads), generator=gen, device="cuda").to(torch.uint8)  # noqa: E731
+    k, v = code(), code()
+    for b, n in enumerate(lens):
+        if n % 64:
+            k[table[b, n // 64], :, n % 64:] = v[table[b, n // 64], :, n % 64:] = 0x7F
+    vt = torch.empty(pages, heads, hd, 64, dtype=torch.uint8, device="cuda")
+    vt[..., slots] = v.transpose(2, 3)
+    return f3c.Cache8(k, vt, scale(), scale(), to_dev(table.astype(np.int32)))
+
+
+def _tokens(torch, pool, b, held, head):
+    """(K, V float64 [held][hd] of a sample's tokens, whether each is there)."""
+    pages, slots = pool.k.shape[0], torch.from_numpy(cache8.SLOTS).cuda()
+    t = pool.table[b, :-(-held // 64)].long()
+    there = (t >= 0) & (t < pages)
+    t = torch.where(there, t, 0)
+
+    def values(codes, scale):
+        x = codes.contiguous().view(torch.float8_e4m3fn).double() * torch.exp2(scale.double() - 127)[:, None, None]
+        return x.reshape(-1, x.shape[-1])[:held]
+
+    return (values(pool.k[t, head], pool.k_scale[t, head]),
+            values(pool.v[t, head][..., slots].transpose(1, 2), pool.v_scale[t, head]), there.repeat_interleave(64)[:held])
+
+
+def _check_rows(torch, f3c, pool, heads, lens, nq, causal, gen, scale=1.5):
+    """As _check_attention, with the float64 softmax in torch on the GPU. Scores here are hundreds apart: exponentials below
+    2^-126 are zero, and they are taken relative to a reference within 2^24 of the largest, so that a token whose share is
+    below 2^-102 of the largest may count as none; held tokens of at most max |v| lose held 2^-102 max |v| in all."""
+    kv, hd = pool.k.shape[1], pool.k.shape[3]
+    off = [2]
+    for n in nq:
+        off.append(off[-1] + n)
+    q = (torch.randn(off[-1] + 1, heads * hd, generator=gen, device="cuda") * scale).bfloat16()
+    o = torch.full_like(q, 5.0)
+    say("attention rows", heads, kv, hd, lens, nq, causal)
+    f3c.op_cache8_attention(pool, heads, off, lens, q, o, causal=causal)
+    torch.cuda.synchronize()
+    assert bool((o[:2] == 5).all()) and bool((o[off[-1]:] == 5).all())
+    for b, held in enumerate(lens):
+        for h in range(heads if held else 0):
+            if h % (heads // kv) == 0:
+                k, v, there = _tokens(torch, pool, b, held, h // (heads // kv))
+                bad_k, bad_v = k.isnan().any(1), v.isnan()
+                k, v = k.nan_to_num(nan=0.0), v.nan_to_num(nan=0.0)
+            for at in range(0, nq[b], 1024):
+                n = min(1024, nq[b] - at)
+                rows, cols = slice(off[b] + at, off[b] + at + n), slice(h * hd, (h + 1) * hd)
+                see = there[None].expand(n, held)
+                if causal:
+                    last = held - nq[b] + at + torch.arange(n, device="cuda")
+                    see = see & (torch.arange(held, device="cuda")[None] <= last[:, None])
+                x = q[rows, cols].double()
+                s = (x @ k.t() / hd ** 0.5).masked_fill(~see, float("-inf"))
+                p = torch.softmax(s, 1).nan_to_num(nan=0.0)
+                want, mag = p @ v, p @ v.abs()
+                top = ((x.abs() @ k.abs().t()) / hd ** 0.5).masked_fill(~see, 0.0).amax(1, keepdim=True)
+                ds = 3 * (hd + 2) * 2.0 ** -24 * top                   # (as in _bounds)
+                tol = (2.0 ** -8 + 2.0 ** -12 + 2 * ds) * mag
+                tol = tol + 2.0 ** -8 * (want.abs() + tol) + held * 2.0 ** -102 * v.abs().max()
+                nan = (see & bad_k).any(1, keepdim=True) | (see.double() @ bad_v.double() > 0)
+                got = o[rows, cols].double()
+                assert torch.equal(got.isnan(), nan), (b, h, at)
+                assert bool(((got - want).abs() <= tol)[~nan].all()), (b, h, at, float(((got - want).abs() / tol)[~nan].max()))
+        if not held:
+            assert bool((o[off[b]:off[b + 1]] == 0).all())
+
+
+# head width, K/V heads, heads, queries, tokens, causal: calls that take 128 and 256 rows a workgroup, their pages in
+# one piece and split, one sample and ragged ones
+ROWS = [(32, 2, 14, [2050], [333], False), (32, 2, 14, [1500, 500, 1, 0, 750], [333, 166, 111, 333, 33], False),
+        (32, 2, 14, [460], [6000], False), (32, 4, 16, [333], [9000], True), (32, 8, 16, [460], [9000], True),
+        (32, 8, 16, [1500, 500, 1, 0, 750], [3000, 1500, 1000, 3000, 2700], True), (32, 4, 16, [4500, 900], [4500, 4600], True),
+        (64, 2, 14, [2050], [333], False), (64, 2, 14, [4500, 1500, 1, 0, 2250], [333, 166, 111, 333, 33], False),
+        (64, 2, 4, [970, 323, 1, 0, 485], [6000, 3000, 2000, 6000, 5700], False), (64, 8, 16, [2050], [6000], False),
+        (64, 2, 14, [333], [9000], True), (64, 8, 16, [460], [9000], True), (64, 8, 16, [3000, 5], [4000, 0], True),
+        (128, 8, 16, [970], [333], False), (128, 2, 4, [3000, 1000, 1, 0, 1500], [333, 166, 111, 333, 33], False),
+        (128, 4, 4, [200, 66, 1, 0, 100], [9000, 4500, 3000, 9000, 8700], False), (128, 2, 14, [1500], [2000], True),
+        (128, 4, 4, [200, 66, 1, 0, 100], [9000, 4500, 3000, 9000, 8700], True), (128, 8, 16, [970, 323], [900, 500], True)]
+
+
+@pytest.mark.parametrize("hd,kv,heads,nq,lens,causal", ROWS)
+def test_attention_rows_against_float64(torch, f3c, hd, kv, heads, nq, lens, causal):
+    gen = torch.Generator(device="cuda").manual_seed(hd + sum(lens))
+    pool = _random_pool(torch, f3c, gen, lens, kv, hd)
+    _check_rows(torch, f3c, pool, heads, lens, nq, causal, gen)
+    # scores far apart, their maxima moving from page to page
+    pool.k_scale[:] = torch.randint(124, 133, pool.k_scale.shape, generator=gen, device="cuda").to(torch.uint8)
+    _check_rows(torch, f3c, pool, heads, lens, nq, causal, gen, scale=4.0)
+    # pages that are none at the front, in the middle, two together, the last; all of a sample's
+    table = pool.table.clone()
+    whole = -(-lens[0] // 64)
+    for at, bad in ((0, -1), (whole // 2, pool.k.shape[0]), (whole // 2 + 1, 2 ** 31 - 1), (whole - 1, -2 ** 31)):
+        pool.table[0, at] = bad
+    if len(lens) > 1:
+        pool.table[1] = -1
+    _check_rows(torch, f3c, pool, heads, lens, nq, causal, gen)
+    pool.table[:] = table
+    # NaN: of K in the last token, which a causal call's last query sees, of V in a column of another head's, 200 before
+    # it, and of V in a token that all queries see
+    def page(b, t):
+        return int(table[b, t // 64]), t % 64
+
+    n = lens[0]
+    (x, t), (y, u), (z, w) = page(0, n - 1), page(0, n - 201), page(0, 1)
+    pool.k[x, 0, t, 5] = 0xFF
+    pool.v[y, kv - 1, 7, cache8.slot(u)] = 0x7F
+    pool.v[z, 0, 9, cache8.slot(w)] = 0x7F
+    _check_rows(torch, f3c, pool, heads, lens, nq, causal, gen)
+
+
 # ----------------------------------------------------------------------------------------------------- together
 
 def test_block_on_8_bits(torch, f3c):
