@@ -485,16 +485,19 @@ __device__ const u32x4 kNoPage[64] = {};
 // compiler's scheduler behind each group; left alone it gathers the products and then the
 // vector work, and both waves of a SIMD wait for the same unit). Pages at a row's limit, at
 // most a few and the last, go one step after the other, with masks.
-template <int HD, int QB, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
+template <int HD, int QB, int NW, int NG>
+__global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
   constexpr int ROWS = 32 * QB * NW, TILE = kPage * HD, STAGES = 5;
   constexpr int NS = HD / 32, NV = HD / 32;        // pairs of K slices of 16 columns; output tiles of 32
   constexpr int CPR = HD / 16;                     // 16-byte chunks of a row of K
   constexpr int DMA = TILE / 1024;                 // DMA instructions per tile
   constexpr int DQ = 2 * DMA / NW;                 // of both tiles, per wave
   static_assert(2 * DMA % NW == 0, "whole DMA blocks per wave");
-  __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * TILE];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int RING = STAGES * 2 * TILE, PARTS = 64 * NW * QB * (HD / 2 + 2) * 4;         // (PARTS: of a group, for the join)
+  static_assert(NG == 1 || PARTS <= NG * RING, "the second group's sums fit");
+  __shared__ __attribute__((aligned(16))) char lds[NG * RING];
+  const int tid = threadIdx.x, lane = tid & 63, of_all = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = of_all % NW, group = of_all / NW;
   const int g = lane >> 5, r32 = lane & 31;
   const Item it = item_of(p);
   const int kvh = p.c.kv_heads, b = it.b, head = it.head, item = it.item;
@@ -527,7 +530,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
                     : p.causal ? max(n - nq + min((row_w + 32 * QB - 1) / p.group, nq - 1) + 1, 0) : n;
   const int lim_hi = p.causal ? max(n - nq + min((row_t + ROWS - 1) / p.group, nq - 1) + 1, 0) : n;
   const int pages = (lim_hi + kPage - 1) / kPage;
-  const int begin = min(it.split * p.split_pages, pages), end = min(begin + p.split_pages, pages);
+  // (a group's pages: as many for each, for the barriers that they meet at; from `held` on they
+  // are none)
+  const int begin0 = min(it.split * p.split_pages, pages), held = min(begin0 + p.split_pages, pages);
+  const int share = (held - begin0 + NG - 1) / NG, begin = begin0 + group * share, end = begin + share;
 
   // o: outputs; m: the reference that probabilities are relative to, base 2; l: sums of a
   // lane's own keys. Where masks apply the reference is moved above 2^8 times it; in whole pages
@@ -553,7 +559,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
   // lanes reading a chunk of 16 rows meet 16 different places of 256 bytes; V: rows of 4.
   auto kswz = [](int row) { return row / (16 / CPR) & (CPR - 1); };
   auto vswz = [](int row) { return row >> 2 & 3; };
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + (uint32_t)(group * RING);
   // A lane's place within the 1 KiB that a DMA instruction reads (the same for all of a
   // wave's: blocks are NW apart, and only their parity enters, of 128 columns alone).
   static_assert(NW % 2 == 0, "a wave's blocks are all even or all odd");
@@ -580,7 +586,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
   auto look = [&](int at) {
     base = at;
     pg = -1;
-    if (at + lane < end) pg = p.c.table[(int64_t)b * p.c.max_pages + at + lane];
+    if (at + lane < held) pg = p.c.table[(int64_t)b * p.c.max_pages + at + lane];
     if ((uint32_t)pg >= (uint32_t)p.c.n_pages) pg = -1;
     const int64_t x = (int64_t)(pg < 0 ? 0 : pg) * kvh + head;
     pks = pg < 0 ? 1.0f : fp8_scale(p.c.ks[x]);
@@ -876,9 +882,51 @@ __global__ __launch_bounds__(64 * NW, 2) void k_cache8_rows(Attn8Args p) {
     }
   }
   wait_vm<0>();                                    // no DMA into LDS that another workgroup may get
+  float sums[QB];
+#pragma unroll
+  for (int j = 0; j < QB; ++j) sums[j] = half_sum(l[j][0]);
+  if constexpr (NG > 1) {                          // the second group's results, into the first's
+    typedef __attribute__((address_space(3))) f32x4 lds_f4;
+    typedef __attribute__((address_space(3))) float lds_f;
+    const uint32_t all = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const uint32_t at4 = all + (uint32_t)((wave * QB * NV * 256 + lane) * 16);
+    const uint32_t at1 = all + (uint32_t)(NW * QB * NV * 4096 + (wave * QB * 128 + lane) * 4);
+    __syncthreads();
+    if (group) {
+#pragma unroll
+      for (int j = 0; j < QB; ++j) {
+#pragma unroll
+        for (int t = 0; t < NV; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *(lds_f4*)(uintptr_t)(at4 + (uint32_t)((j * NV + t) * 4096 + e * 256)) =
+                f32x4{o[j][t][e], o[j][t][e + 1], o[j][t][e + 2], o[j][t][e + 3]};
+        *(lds_f*)(uintptr_t)(at1 + (uint32_t)(j * 512)) = m[j];
+        *(lds_f*)(uintptr_t)(at1 + (uint32_t)(j * 512 + 256)) = sums[j];
+      }
+    }
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+      const float m1 = *(lds_f*)(uintptr_t)(at1 + (uint32_t)(j * 512)), top = fmaxf(m[j], m1);
+      const float f0 = m[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[j] - top);
+      const float f1 = m1 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m1 - top);
+      m[j] = top;
+      sums[j] = sums[j] * f0 + *(lds_f*)(uintptr_t)(at1 + (uint32_t)(j * 512 + 256)) * f1;
+#pragma unroll
+      for (int t = 0; t < NV; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const f32x4 v = *(lds_f4*)(uintptr_t)(at4 + (uint32_t)((j * NV + t) * 4096 + e * 256));
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][t][e + x] = o[j][t][e + x] * f0 + v[x] * f1;
+        }
+    }
+  }
 #pragma unroll
   for (int j = 0; j < QB; ++j) {
-    const float sum = half_sum(l[j][0]);
+    const float sum = sums[j];
     int again = r32 + 32 * j, tok, col;
     asm("" : "+v"(again));
     place(again, tok, col);
@@ -948,7 +996,7 @@ __global__ __launch_bounds__(256) void k_cache8_join(Attn8Args p) {
 struct Plan {
   Segs tiles, items;
   uint8_t order[kMaxBatch];
-  int rows, split_pages;                           // rows: of a tile
+  int rows, groups, split_pages;                   // rows: of a tile; groups: that share a tile's pages
   bool split;                                      // some sample's pages are split
   size_t bytes(const Cache8& c) const {
     return split ? (size_t)items.off[items.B] * c.kv_heads * rows * (c.hd + 2) * 4 : 0;
@@ -958,17 +1006,23 @@ struct Plan {
 // What a form of the kernel takes, in us on MI355X: a page of one workgroup's rows while a CU has
 // one of them (first) or more (page, each), and what a workgroup costs beside its pages (own).
 // Of 16 rows, page is a CU's throughput and first the time from page to page of one wave.
-// Measured: 32, 64 and 128 columns, 16 heads, 2048 to 32768 queries over 16384 keys and 32 to 32768
-// over 1374; the pick is within 10% of the best of the forms and splits measured there.
+// Fitted to 33000 timings of all forms and up to 64 splits over 3060 calls (1 to 32 samples of 64 to
+// 40000 tokens, 1 to 9000 queries, 1 to 16 key heads, groups of 1 to 7, causal or not): the
+// pick takes 1% longer than the best of them in the mean, 6% or less in 95 of 100 calls, 32% at
+// worst (ragged calls of a few pieces for each CU).
 struct FormCost {
-  int rows, hd;
+  int rows, hd, groups;
   double first, page, own;
 };
 constexpr FormCost kForms[] = {
-    {16, 32, 1.0, 0.09, 0.3},  {16, 64, 1.3, 0.14, 0.3},   {16, 128, 3.0, 0.37, 0.4},  {128, 32, 0.7, 0.42, 1.6},
-    {128, 64, 0.95, 0.6, 1.6}, {128, 128, 1.16, 1.1, 3.0}, {256, 32, 0.94, 0.9, 3.0},  {256, 64, 1.25, 1.13, 3.0},
+    {16, 32, 1, 0.78, 0.101, 0.35}, {16, 64, 1, 1.32, 0.155, 0.53}, {16, 128, 1, 2.99, 0.431, 1.23},
+    {128, 32, 1, 0.97, 0.425, 0.63}, {128, 64, 1, 0.92, 0.658, 1.3}, {128, 128, 1, 1.38, 1.075, 3.5},
+    {128, 32, 2, 0.61, 0.447, 1.5}, {128, 64, 2, 0.63, 0.772, 3.3}, {128, 128, 2, 0.96, 1.229, 7.5},
+    {256, 32, 1, 1.05, 0.893, 2.1}, {256, 64, 1, 1.63, 1.101, 3.3},
+    {256, 32, 2, 0.82, 0.903, 3.3}, {256, 64, 2, 0.97, 1.171, 4.7},
 };
-constexpr double kLaunchUs = 5.0, kJoinUs = 5.0, kPartialBytesPerUs = 4e6, kReadBytesPerUs = 5e6;
+constexpr double kLaunchUs = 5.5, kJoinUs = 3.0, kJoinSplitUs = 0.29, kPartialBytesPerUs = 7.5e6, kReadBytesPerUs = 5e6;
+constexpr double kSplitRounds = 1.1;               // splits of what fills the CUs without: partial results in their way
 constexpr int kLeastSplit = 8;                     // pages
 
 Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool causal, size_t ws_bytes) {
@@ -982,6 +1036,8 @@ Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool ca
     most_rows = std::max(most_rows, (int64_t)(rows.off[b + 1] - rows.off[b]) * group);
   }
   std::stable_sort(best.order, best.order + B, [&](int x, int y) { return pages[x] > pages[y]; });
+  bool ragged = causal;                            // pieces of different length
+  for (int b = 1; b < B; ++b) ragged = ragged || len.n[b] != len.n[0];
   int longest = 1;
   for (int y = B - 1; y >= 0; --y)
     if (rows.off[best.order[y] + 1] > rows.off[best.order[y]]) longest = std::max(pages[best.order[y]], 1);
@@ -989,12 +1045,16 @@ Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool ca
   for (const FormCost& f : kForms) {
     if (f.hd != c.hd || (f.rows > 16 && most_rows <= 16)) continue;
     int tiles[kMaxBatch];
-    double work = 0.0, read = 0.0;                 // pages of all tiles and heads; bytes
+    double work = 0.0, read = 0.0, whole = 0.0;    // pages of all tiles and heads; bytes; items without splits
     for (int y = 0; y < B; ++y) {
       const int b = best.order[y], nq = rows.off[b + 1] - rows.off[b];
       tiles[y] = (int)(((int64_t)nq * group + f.rows - 1) / f.rows);
-      const double seen = pages[b] - (causal ? std::min(nq, len.n[b]) / (2.0 * kPage) : 0.0);
+      const double unseen = !causal || !nq ? 0.0                       // in the mean of its rows
+                            : nq <= len.n[b] ? nq / (2.0 * kPage)
+                                             : pages[b] - pages[b] * (double)len.n[b] / (2.0 * nq);
+      const double seen = pages[b] - unseen;
       work += tiles[y] * std::max(seen, 0.5) * c.kv_heads;
+      whole += (double)tiles[y] * c.kv_heads;
       if (tiles[y]) read += 2.0 * pages[b] * kPage * c.hd * c.kv_heads;
     }
     for (int k = 1; k <= 128; k = k < 4 ? k + 1 : k * 2) {
@@ -1012,14 +1072,23 @@ Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool ca
       } else if (per_cu <= 1.0) {
         t = p * f.first + f.own;
       } else {
-        // whole rounds, or pieces of different length, the longest first
-        const double uneven = causal ? 0.35 * p : (std::ceil(per_cu) / per_cu - 1.0) * 0.5 * load;
-        t = std::max(p * f.first, (load + uneven) * f.page) + per_cu * f.own;
+        double longest_cu;                         // pages of the CU that has most
+        if (ragged) {
+          // lengths evenly from p down to `least`: one workgroup at a time, the 256th and the next
+          // share a CU; two at a time, the first and the 257th
+          const double mean = load / per_cu, least = std::max(2.0 * mean - p, 0.0), next = p - (p - least) / per_cu;
+          longest_cu = std::max(f.groups > 1 ? 2.0 * next : p + next, load + (f.groups > 1 ? 0.33 : 0.38) * mean);
+        } else {
+          longest_cu = load * (1.0 + (std::ceil(per_cu) / per_cu - 1.0) * (f.groups > 1 ? 0.89 : 0.97));
+        }
+        t = std::max(p * f.first, longest_cu * f.page) + per_cu * f.own;
       }
-      t += kLaunchUs + (k > 1 ? kJoinUs + 2.0 * need / kPartialBytesPerUs : 0.0);
+      t += kLaunchUs + (k > 1 ? kJoinUs + kJoinSplitUs * k + 2.0 * need / kPartialBytesPerUs : 0.0);
+      if (k > 1 && f.rows > 16 && whole > 256.0) t *= kSplitRounds;
       if (best_t == 0.0 || t < best_t) {
         best_t = t;
         best.rows = f.rows;
+        best.groups = f.groups;
         best.split_pages = p;
       }
     }
@@ -1036,13 +1105,19 @@ Plan plan(const Cache8& c, int heads, const Segs& rows, const Lens& len, bool ca
   return best;
 }
 
+template <int HD, int QB>
+void launch_rows(const Attn8Args& a, const Plan& pl, uint32_t items, hipStream_t s) {
+  if (pl.groups == 2) launch((k_cache8_rows<HD, QB, 4, 2>), dim3(items), dim3(512), 0, s, a);
+  else launch((k_cache8_rows<HD, QB, 4, 1>), dim3(items), dim3(256), 0, s, a);
+}
+
 template <int HD>
 hipError_t launch_attn8(const Attn8Args& a, const Plan& pl, hipStream_t s) {
   const int64_t items = (int64_t)a.items.off[a.items.B] * a.c.kv_heads;
   if (!items) return hipSuccess;
   if (pl.rows == 256) {
-    if constexpr (HD < 128) launch((k_cache8_rows<HD, 2, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
-  } else if (pl.rows == 128) launch((k_cache8_rows<HD, 1, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
+    if constexpr (HD < 128) launch_rows<HD, 2>(a, pl, (uint32_t)items, s);
+  } else if (pl.rows == 128) launch_rows<HD, 1>(a, pl, (uint32_t)items, s);
   else if (items <= 256) launch((k_cache8_attn<HD, 8>), dim3((uint32_t)items), dim3(512), 0, s, a);
   else launch((k_cache8_attn<HD, 4>), dim3((uint32_t)items), dim3(256), 0, s, a);
   if (pl.split) {

@@ -409,7 +409,24 @@ ROWS = [(32, 2, 14, [2050], [333], False), (32, 2, 14, [1500, 500, 1, 0, 750], [
         (64, 2, 14, [333], [9000], True), (64, 8, 16, [460], [9000], True), (64, 8, 16, [3000, 5], [4000, 0], True),
         (128, 8, 16, [970], [333], False), (128, 2, 4, [3000, 1000, 1, 0, 1500], [333, 166, 111, 333, 33], False),
         (128, 4, 4, [200, 66, 1, 0, 100], [9000, 4500, 3000, 9000, 8700], False), (128, 2, 14, [1500], [2000], True),
-        (128, 4, 4, [200, 66, 1, 0, 100], [9000, 4500, 3000, 9000, 8700], True), (128, 8, 16, [970, 323], [900, 500], True)]
+        (128, 4, 4, [200, 66, 1, 0, 100], [9000, 4500, 3000, 9000, 8700], True), (128, 8, 16, [970, 323], [900, 500], True),
+        # and calls whose pages two groups of waves share, or do not
+        (32, 8, 16, [2050], [333], False), (32, 2, 14, [1500], [2000], False), (32, 8, 16, [700], [6000], True),
+        (32, 8, 16, [700, 233, 1, 0, 350], [3000, 1500, 1000, 3000, 2700], True), (32, 2, 4, [4500], [3000], False),
+        (32, 2, 4, [970, 323, 1, 0, 485], [9000, 4500, 3000, 9000, 8700], True), (32, 2, 14, [4500], [1000], False),
+        (32, 8, 16, [970], [4000], False), (32, 8, 16, [460, 153, 1, 0, 230], [9000, 4500, 3000, 9000, 8700], True),
+        (32, 8, 16, [2050], [3000], False),
+        (64, 16, 16, [700, 233, 1, 0, 350], [4000, 2000, 1333, 4000, 3700], False), (64, 2, 4, [2050], [6000], True),
+        (64, 2, 14, [2050, 683, 1, 0, 1025], [3000, 1500, 1000, 3000, 2700], True),
+        (64, 16, 16, [4500, 1500, 1, 0, 2250], [500, 250, 166, 500, 200], False), (64, 8, 16, [2050], [6000], True),
+        (64, 2, 14, [1500], [500], False), (64, 2, 14, [2050], [3000], True), (64, 2, 14, [460], [4000], True),
+        (64, 2, 4, [970, 323, 1, 0, 485], [4000, 2000, 1333, 4000, 3700], True), (64, 8, 16, [2050], [700], False),
+        (64, 2, 14, [4500], [6000], True), (64, 8, 16, [333], [9000], True),
+        (64, 2, 4, [4500, 1500, 1, 0, 2250], [1374, 687, 458, 1374, 1074], False),
+        (128, 1, 1, [4500], [2000], False), (128, 2, 14, [200, 66, 1, 0, 100], [2000, 1000, 666, 2000, 1700], True),
+        (128, 8, 16, [2050, 683, 1, 0, 1025], [3000, 1500, 1000, 3000, 2700], True), (128, 2, 14, [970], [700], False),
+        (128, 1, 1, [2050], [6000], False), (128, 2, 4, [333, 111, 1, 0, 166], [6000, 3000, 2000, 6000, 5700], True),
+        (128, 8, 16, [700, 233, 1, 0, 350], [1000, 500, 333, 1000, 700], True), (128, 2, 14, [333], [3000], True)]
 
 
 @pytest.mark.parametrize("hd,kv,heads,nq,lens,causal", ROWS)
