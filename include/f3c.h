@@ -499,7 +499,8 @@ int f3c_op_cache8_append(const f3c_cache8* cache, int32_t dtype, int32_t batch, 
  * sqrt(head_dim)) V. causal: a sample's queries are its last tokens, query i of n seeing
  * tokens 0..len - n + i. A query that sees no token gets zeros. q_prescaled as in
  * f3c_op_attention. Any finite scores; tiles' values between 2^-100 and 2^100 in
- * magnitude. NaN in a token reaches the queries that see it and no others. workspace
+ * magnitude (a token whose share is below 2^-102 of the row's largest may count as none).
+ * NaN in a token reaches the queries that see it and no others. workspace
  * (device, 16-byte aligned, may be NULL): the key range is split over workgroups where
  * there are few queries, as far as the workspace holds the splits' results;
  * f3c_op_cache8_attention_bytes says how much the call makes use of (it looks at no device
