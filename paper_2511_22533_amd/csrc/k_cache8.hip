@@ -513,7 +513,8 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
   constexpr int DMA = TILE / 1024;                 // DMA instructions per tile
   constexpr int DQ = 2 * DMA / NW;                 // of both tiles, per wave
   static_assert(2 * DMA % NW == 0, "whole DMA blocks per wave");
-  constexpr int RING = STAGES * 2 * TILE, PARTS = 64 * NW * QB * (HD / 2 + 2) * 4;         // (PARTS: of a group, for the join)
+  constexpr int RING = STAGES * 2 * TILE;
+  constexpr int PARTS = 64 * NW * QB * (HD / 2 + 2) * 4;               // a group's results, for the join
   static_assert(NG == 1 || PARTS <= NG * RING, "the second group's sums fit");
   __shared__ __attribute__((aligned(16))) char lds[NG * RING];
   const int tid = threadIdx.x, lane = tid & 63, of_all = __builtin_amdgcn_readfirstlane(tid >> 6);

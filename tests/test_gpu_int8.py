@@ -62,6 +62,16 @@ def test_quant_bit_exact(torch, f3c, dtype, rows, K, pad):
     _check_quant(torch, f3c, _view(torch, x, pad, 0, t)[1], pad)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [120, 128, 256, 264, 512, 1024, 1032, 1600, 2048, 4096, 4104])
+def test_quant_at_the_borders_of_its_forms(torch, f3c, dtype, K):
+    say("quant_i8 forms", dtype, K)
+    rng = np.random.default_rng(K)
+    x = rng.standard_normal((37, K)).astype(np.float32)
+    x[5, K - 1], x[6, K - 1], x[7], x[8, 0] = 100.0, np.nan, 0.0, -np.inf
+    _check_quant(torch, f3c, _view(torch, x, 8, 0, torch.float32 if dtype == "f32" else torch.bfloat16)[1], 8)
+
+
 @pytest.mark.parametrize("K", [64, 512, 8448])
 def test_quant_borders(torch, f3c, K):
     """Quotients at half steps and next to them: rows whose largest value is 127 of a scale, the rest at (n + 1/2) times
