@@ -13,6 +13,7 @@ import ctypes
 import functools
 import os
 import re
+from array import array
 from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -109,11 +110,11 @@ _SIGS = {
     "f3c_op_quant_i8": (c_int, [c_int, c_int, c_int, c_p, c_int, c_p, c_int, c_p, c_p]),
     "f3c_op_gemm_i8": (c_int, [c_int, c_int, c_int, c_int, c_p, c_int, c_p, c_p, c_int, c_p, c_p, c_p, c_p, c_int, c_p,
                                c_int, c_p]),
-    "f3c_op_cache8_append": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, P_i32, P_i32, c_p, c_int, c_p, c_int,
+    "f3c_op_cache8_append": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, c_p, c_p, c_p, c_int, c_p, c_int,
                                      c_p]),
-    "f3c_op_cache8_attention_bytes": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, P_i32, P_i32, c_int,
+    "f3c_op_cache8_attention_bytes": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, c_p, c_p, c_int,
                                               ctypes.POINTER(c_sz)]),
-    "f3c_op_cache8_attention": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, P_i32, P_i32, c_p, c_int, c_p, c_int,
+    "f3c_op_cache8_attention": (c_int, [ctypes.POINTER(Cache8Args), c_int, c_int, c_p, c_p, c_p, c_int, c_p, c_int,
                                         c_int, c_int, c_p, c_sz, c_p]),
     "f3c_op_modulation": (c_int, [c_p, c_d, c_p, c_p, c_p]),
     "f3c_op_embed": (c_int, [c_p, c_int, c_p, c_p, P_i32, c_p, c_p]),
@@ -740,22 +741,20 @@ def _cache8(cache, batch: int, dev: int, T):
                      "[pages][heads], table int32 [samples][pages of one], contiguous on the current GPU expected")
 
 
-@functools.lru_cache(maxsize=None)
-def _int_array(n: int):
-    return ctypes.c_int32 * n
-
-
 def _ints(values):
-    """Host integers of a call as the C array, made at each call (they change from token to token)."""
+    """Host integers of a call as a C array, made at each call (they change from token to token)."""
     try:
-        return _int_array(len(values))(*values)
-    except TypeError:                              # NumPy's integers, elements of tensors
-        return _i32(values)
+        return array("i", values)
+    except TypeError:                              # elements that are no integers by type
+        return array("i", [int(v) for v in values])
 
 
 def _samples(off, lens, rows: int):
-    """(row offsets, samples, tokens held) as C values; the library looks at their order."""
-    offsets, held = _ints(off), _ints(lens)
+    """(row offsets, samples, tokens held), as arrays; the library looks at their order."""
+    try:
+        offsets, held = _ints(off), _ints(lens)
+    except OverflowError:
+        raise ValueError("off, lens: 32-bit integers expected") from None
     B = len(held)
     if B < 1 or len(offsets) != B + 1 or offsets[0] < 0 or offsets[B] > rows:
         raise ValueError("off: B + 1 row offsets within the rows, lens: B token counts expected")
@@ -773,7 +772,7 @@ def op_cache8_append(dtype: int, cache, lens: Sequence[int], off: Sequence[int],
     offsets, B, held = _samples(off, lens, R)
     args, heads, hd = _cache8(cache, B, dev, T)
     check((_lib or lib()).f3c_op_cache8_append(
-        args, dtype, B, held, offsets, *_rows("k", k, T[dtype], R, heads * hd, dev),
+        args, dtype, B, held.buffer_info()[0], offsets.buffer_info()[0], *_rows("k", k, T[dtype], R, heads * hd, dev),
         *_rows("v", v, T[dtype], R, heads * hd, dev), _stream_on(stream, dev, T["torch"])))
 
 
@@ -790,9 +789,10 @@ def op_cache8_attention(cache, heads: int, q_off: Sequence[int], lens: Sequence[
     offsets, B, held = _samples(q_off, lens, R)
     args, _, hd = _cache8(cache, B, dev, T)
     L, on = _lib or lib(), _stream_on(stream, dev, torch)
+    off_at, held_at = offsets.buffer_info()[0], held.buffer_info()[0]
     if workspace is None:
         need = c_sz()
-        check(L.f3c_op_cache8_attention_bytes(args, heads, B, offsets, held, int(causal), need))
+        check(L.f3c_op_cache8_attention_bytes(args, heads, B, off_at, held_at, int(causal), need))
         if need.value and stream is None:
             workspace = torch.empty(need.value, dtype=torch.uint8, device=q.device)
         elif need.value:
@@ -803,7 +803,7 @@ def op_cache8_attention(cache, heads: int, q_off: Sequence[int], lens: Sequence[
         raise ValueError("workspace: a contiguous tensor on the current GPU expected")
     ws, size = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     bf16 = T[F3C_BF16]
-    check(L.f3c_op_cache8_attention(args, heads, B, offsets, held, *_rows("q", q, bf16, R, heads * hd, dev),
+    check(L.f3c_op_cache8_attention(args, heads, B, off_at, held_at, *_rows("q", q, bf16, R, heads * hd, dev),
                                     *_rows("o", o, bf16, R, heads * hd, dev), int(causal), int(q_prescaled), ws, size, on))
 
 

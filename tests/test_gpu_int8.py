@@ -229,6 +229,22 @@ def test_gemm_far_rows(torch, f3c):
     assert np.all(np.abs(out.float().cpu().numpy() - want) <= 2.0 ** -7 * np.abs(want) + 1e-6)
 
 
+@pytest.mark.parametrize("M,N", [(700, 512), (5, 528)])
+def test_gemm_far_rows_of_each_kernel(torch, f3c, M, N):
+    """As above where tiles are taken, and of the weights where rows are few."""
+    K, ld = 256, (1 << 22) - 16
+    few = M < 16
+    far = torch.zeros(N if few else M, ld, dtype=torch.int8, device="cuda")[:, :K]
+    a, sa, w, sw, bias = _operands(M, N, K, 3)
+    far.copy_(to_dev(w if few else a))
+    out = torch.zeros(M, 1 << 21, dtype=torch.bfloat16, device="cuda")[:, :N]
+    say("gemm_i8 far rows", M, N)
+    f3c.op_gemm_i8(0, *((to_dev(a), to_dev(sa), far, to_dev(sw)) if few else (far, to_dev(sa), to_dev(w), to_dev(sw))),
+                   to_dev(bias), out=out)
+    want = int8.linear(a, sa, w, sw, bias)
+    assert np.all(np.abs(out.float().cpu().numpy() - want) <= 2.0 ** -7 * np.abs(want) + 1e-6)
+
+
 def test_quantised_product_chain_and_graph(torch, f3c):
     """Rows through quantisation, an MLP's two products and the residual, eagerly, on another stream and from a graph
     replayed with new inputs between eager work."""

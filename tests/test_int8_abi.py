@@ -2,6 +2,7 @@
 GPU needed: the pointers here are host addresses that nothing reads)."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from paper_2511_22533_amd import f3c
@@ -168,3 +169,30 @@ def test_bindings_look_at_the_cache(monkeypatch):
     for off, lens in (([0, 2], [4]), ([-1, 1], [4]), ([0, 1], [4, 4]), ([0], [])):
         with pytest.raises(ValueError, match="off"):
             f3c.op_cache8_attention(f3c.Cache8(**good), 2, off, lens, q, q)
+
+
+def test_host_lists_of_any_integers(monkeypatch):
+    """Lengths and offsets as lists, tuples, NumPy arrays, elements of tensors: the values at the call; none that 32 bits
+    do not hold."""
+    import torch
+    got = []
+
+    class Library:
+        def f3c_op_cache8_append(self, args, dtype, batch, held, off, *rest):
+            got.append([list((ctypes.c_int32 * n).from_address(a)) for a, n in ((held, batch), (off, batch + 1))])
+            return f3c.F3C_OK
+
+    monkeypatch.setattr(f3c, "_lib", Library())
+    monkeypatch.setattr(f3c, "_device", lambda t, torch: t.get_device())
+    monkeypatch.setattr(f3c, "_stream_on", lambda *a: 0)
+    e = lambda *s, t=torch.uint8: torch.empty(*s, dtype=t)  # noqa: E731
+    cache = f3c.Cache8(e(3, 2, 64, 32), e(3, 2, 32, 64), e(3, 2), e(3, 2), e(2, 3, t=torch.int32))
+    k = e(4, 64, t=torch.bfloat16)
+    for lens, off in (([5, 0], [0, 1, 4]), ((5, 0), (0, 1, 4)), (np.array([5, 0]), np.array([0, 1, 4], np.int64)),
+                      ([np.int32(5), torch.tensor(0)], torch.tensor([0, 1, 4]))):
+        f3c.op_cache8_append(f3c.F3C_BF16, cache, lens, off, k, k)
+    assert got == [[[5, 0], [0, 1, 4]]] * 4
+    for lens, off in (([2 ** 32 + 5, 0], [0, 1, 4]), ([5, 0], [0, 1, 2 ** 32 + 4]), ([5, -2 ** 31 - 1], [0, 1, 4])):
+        with pytest.raises(ValueError, match="32-bit"):
+            f3c.op_cache8_append(f3c.F3C_BF16, cache, lens, off, k, k)
+    assert len(got) == 4
