@@ -660,7 +660,8 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
       fence();
     }
   };
-  // A page with masks, one step after the other.
+  // A page with masks, one step after the other; none for keys behind all of the wave's limits
+  // (1374 tokens end 30 into a page: 32768 queries 244 -> 235 us).
   auto masked_page = [&](int i, uint32_t at, float ks, float vs) __attribute__((always_inline)) {
     // (tokens counted from the lane's first; opaque, or the compiler keeps 64 sums over all pages)
     int there = n - i * kPage - 4 * g, seen[QB];
@@ -671,7 +672,7 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
       asm("" : "+v"(seen[j]));
     }
 #pragma unroll 1
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2 && i * kPage + 32 * h < lim_w; ++h) {
       f32x16 s[QB];
       scores(at + (uint32_t)(h * 32 * HD), ks, s);
       u32x4 pf[QB][2];
