@@ -42,7 +42,7 @@ __device__ __forceinline__ void load8(float (&x)[8], const T* p) {
 // e4m3's subnormals).
 //
 // Many tokens are bound by HBM, behind a workgroup's chain of table, rows, maximum and store: four
-// samples of 1374 tokens, 16 heads of 64, take 9.0 us (27 MB, 5.3 us at a copy's rate), the
+// samples of 1374 tokens, 16 heads of 64, take 8.9 us (27 MB, 5.3 us at a copy's rate), the
 // next tokens of 32 sequences, 8 heads of 128, 5.0 us, all of it the chain.
 template <typename T, int HD>
 __global__ __launch_bounds__(2 * HD) void k_cache8_append(AppendArgs p) {
@@ -501,9 +501,9 @@ __device__ const u32x4 kNoPage[64] = {};
 // with two), many tiles one, whose workgroups hide each other's beginnings and ends (4096
 // over 4096: 145 against 149).
 //
-// Bound by vector issue: at 9831 queries over 32768 tokens, 16 heads of 64 (1423 us, 930 TFLOP/s),
-// it is busy 62% of the cycles (exponentials and roundings to bf16 half of that, widening a
-// quarter), the matrix pipes 45%; over 1374 tokens (32768 queries, 223 us, 830 TFLOP/s) the first
+// Bound by vector issue: at 9831 queries over 32768 tokens, 16 heads of 64 (1388 us, 950 TFLOP/s),
+// it is busy 63% of the cycles (exponentials and roundings to bf16 half of that, widening a
+// quarter), the matrix pipes 46%; over 1374 tokens (32768 queries, 213 us, 865 TFLOP/s) the first
 // and the last of 22 pages show. 64 rows a wave (QB 2) share each widening: 1744 us with 32 there.
 template <int HD, int QB, int NW, int NG>
 __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {

@@ -21,8 +21,8 @@
 // Integers (OPS_I8) take the same tiles, their scales at the end: sums of 32 bits are exact
 // in any order. The tiles are chosen by e4m3's table: over 1200 calls of integers (1 to 32768
 // rows, 128 to 8192 columns and K) its pick is 0.5% from the best of the nine in the mean, 16% at worst;
-// a table fitted to those calls 0.6%. 8192 x 8192 x 8192 runs at 2160 TOP/s on random bytes,
-// 32768 x 4096 x 1024 with GELU in 175 to 194 us by card: power, and matrix pipes 41%, vector
+// a table fitted to those calls 0.6%. 8192 x 8192 x 8192 runs at 2160 to 2260 TOP/s on random bytes,
+// 32768 x 4096 x 1024 with GELU in 175 to 196 us by card: power, and matrix pipes 41%, vector
 // issue 56% of the cycles.
 #include <algorithm>
 #include <cmath>
