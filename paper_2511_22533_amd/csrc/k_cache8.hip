@@ -215,7 +215,9 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 //
 // Single queries of long sequences are bound by HBM: 32 of up to 16384 tokens, 8 key heads of
 // 128, 32 query heads, 147 us, 5.1 TB/s; a short one by latency: 16 heads of 64, 1374 tokens
-// 7.6 us. Eight waves where workgroups do not fill the CUs, or else four.
+// 7.6 us. Eight waves up to a workgroup for each CU, beyond that four: over 1374 tokens of 64
+// columns 16 workgroups take 8.1 us with eight and 8.7 with four, 256 9.6 and 10.7, 304 14.4 and
+// 12.0, 512 17.4 and 15.5.
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, HD == 128 ? 2 : 3) void k_cache8_attn(Attn8Args p) {
   constexpr int NK = HD / 32, NV = HD / 16;        // K slices of 32 columns; output tiles of 16
