@@ -542,3 +542,36 @@ def test_streams_and_graphs(torch, f3c):
         torch.cuda.synchronize()
         step(o)
         assert torch.equal(o, outs[0]) and torch.equal(o, outs[1]), i
+
+
+@pytest.mark.parametrize("hd,kv,heads,nq,lens", [(64, 8, 16, [333], [9000]), (128, 4, 4, [200, 66, 1, 0, 100], [9000, 4500, 3000, 9000, 8700]),
+                                                 (32, 2, 4, [970, 323], [9000, 4500])])
+def test_rows_at_once_and_replayed(torch, f3c, hd, kv, heads, nq, lens):
+    """Calls of many rows whose pages are split: two streams at once, each with memory of its own, and a graph replayed
+    between them, bit for bit the same."""
+    gen = torch.Generator(device="cuda").manual_seed(hd)
+    pool = _random_pool(torch, f3c, gen, lens, kv, hd)
+    off = [0] + [int(x) for x in np.cumsum(nq)]
+    q = torch.randn(off[-1], heads * hd, generator=gen, device="cuda").bfloat16()
+    outs = [torch.empty_like(q) for _ in range(4)]
+    say("rows at once", hd, heads, nq, lens)
+
+    def call(o):
+        f3c.op_cache8_attention(pool, heads, off, lens, q, o, causal=True)
+
+    call(outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[1])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for o in outs[1:]:
+            o.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        for s, o in zip(streams, outs[2:]):
+            with torch.cuda.stream(s):
+                call(o)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, outs[0]) for o in outs[1:])
