@@ -685,11 +685,13 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
           if (8 * (e / 4) + e % 4 >= seen[j]) s[j][e] = -INFINITY;
         const float mx = half_max(max16(s[j])) * p.scale;
         if (__any(mx > m[j] + 8.0f)) rescale(j, fmaxf(m[j], mx));
-        const float ref = m[j] == -INFINITY ? 0.0f : -m[j];
+        // (the product rounded as the reference was: what an fma leaves of a score of 2^33 is 2^8, and
+        // the largest key's probability 0 or infinite)
+        const float ref = m[j] == -INFINITY ? 0.0f : m[j];
 #pragma unroll
         for (int e = 0; e < 16; e += 2)
-          pf[j][e / 8][e / 2 % 4] = pack2(__builtin_amdgcn_exp2f(__builtin_fmaf(s[j][e], p.scale, ref)),
-                                          __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][e + 1], p.scale, ref)));
+          pf[j][e / 8][e / 2 % 4] = pack2(__builtin_amdgcn_exp2f(s[j][e] * p.scale - ref),
+                                          __builtin_amdgcn_exp2f(s[j][e + 1] * p.scale - ref));
 #pragma unroll
         for (int u = 0; u < 2; ++u) l[j] = row_sum(__builtin_bit_cast(bf16x8, pf[j][u]), l[j]);
         fence();
