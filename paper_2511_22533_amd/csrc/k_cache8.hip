@@ -565,7 +565,11 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
   // (Rounding is relative, so a reference far below the maximum costs nothing; sums of 2^24
   // leave outputs of values up to 2^100 within range. What is below 2^-102 of a row's largest
   // probability may count as none: exponentials end at 2^-126.)
-  constexpr float kMost = 0x1p24f;
+  // Whole pages take their exponents by one fma, which rounds s c - m once, where m is a
+  // rounded s c: the largest key's is half a step of m off 0. Up to kNear that is 2^-1 at most, so
+  // that a step behind a moved reference adds less than 2^14 and is kept; rows further out
+  // (finite: infinite scores are NaN in any way) take their pages one step after the other.
+  constexpr float kMost = 0x1p24f, kNear = 0x1p23f;
   f32x16 o[QB][NV];
   float m[QB];
   f32x4 l[QB];
@@ -662,19 +666,20 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
       fence();
     }
   };
-  // A page with masks, one step after the other; none for keys behind all of the wave's limits
+  // A page with masks (or its second half), one step after the other; none for keys behind all of the wave's limits
   // (1374 tokens end 30 into a page: 32768 queries 244 -> 235 us).
-  auto masked_page = [&](int i, uint32_t at, float ks, float vs) __attribute__((always_inline)) {
+  auto masked_page = [&](int i, int half, uint32_t at, float ks, float vs) __attribute__((always_inline)) {
     // (tokens counted from the lane's first; opaque, or the compiler keeps 64 sums over all pages)
-    int there = n - i * kPage - 4 * g, seen[QB];
+    const int from = i * kPage + 32 * half + 4 * g;
+    int there = n - from, seen[QB];
     asm("" : "+v"(there));
 #pragma unroll
     for (int j = 0; j < QB; ++j) {
-      seen[j] = lim[j] - i * kPage - 4 * g;
+      seen[j] = lim[j] - from;
       asm("" : "+v"(seen[j]));
     }
 #pragma unroll 1
-    for (int h = 0; h < 2 && i * kPage + 32 * h < lim_w; ++h) {
+    for (int h = half; h < 2 && i * kPage + 32 * h < lim_w; ++h) {
       f32x16 s[QB];
       scores(at + (uint32_t)(h * 32 * HD), ks, s);
       u32x4 pf[QB][2];
@@ -684,7 +689,7 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
         for (int e = 0; e < 16; ++e)
           if (8 * (e / 4) + e % 4 >= seen[j]) s[j][e] = -INFINITY;
         const float mx = half_max(max16(s[j])) * p.scale;
-        if (__any(mx > m[j] + 8.0f)) rescale(j, fmaxf(m[j], mx));
+        if (__any(mx - m[j] > 8.0f)) rescale(j, fmaxf(m[j], mx));      // (a difference: m + 8 may be m)
         // (the product rounded as the reference was: what an fma leaves of a score of 2^33 is 2^8, and
         // the largest key's probability 0 or infinite)
         const float ref = m[j] == -INFINITY ? 0.0f : m[j];
@@ -838,24 +843,30 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
     auto after = [&](int s) { return s == STAGES - 1 ? 0 : s + 1; };
     // Pages that all of the wave's rows see, in half steps. A segment of them ends where the
     // reference has to move (a branch within the loop would copy the outputs at every step):
-    // it starts with scores of its own and no probabilities before them.
+    // it starts with scores of its own and no probabilities before them. Where a reference is
+    // beyond kNear, the rest of the pages looked up go like those with masks.
     const int whole = row_w >= nq * p.group ? first : min(max(lim_lo / kPage, first), last);
     int t = 2 * first;
     while (t < 2 * whole) {
-      f32x16 s0[QB], s1[QB];
-      u32x4 p0[QB][2], p1[QB][2];                  // (pairs, as bf16)
-#pragma unroll
-      for (int j = 0; j < QB; ++j) p1[j][0] = p1[j][1] = u32x4{0, 0, 0, 0};
       int i = t / 2;
-      uint32_t vat = at_stage(stage) + (uint32_t)(8 * (t % 2));      // (zeros times V of this page, which every row sees)
-      float vsb = lane_f(pvs, i - base);
+      f32x16 s0[QB];
       scores(at_stage(stage) + (uint32_t)(32 * HD * (t % 2)), lane_f(pks, i - base), s0);
+      bool far = false;
 #pragma unroll
       for (int j = 0; j < QB; ++j) {
         const float mx = half_max(max16(s0[j])) * p.scale, sum = half_sum(l[j][0]);
         if (!none(i) && __any(mx > m[j] + 8.0f || sum > 0x1p12f))
           rescale(j, fmaxf(fmaxf(m[j], mx), m[j] + __builtin_amdgcn_logf(sum)));
+        const float off = __builtin_fabsf(m[j]);
+        far = far || (off > kNear && off < INFINITY);
       }
+      if (__any(far)) break;
+      f32x16 s1[QB];
+      u32x4 p0[QB][2], p1[QB][2];                  // (pairs, as bf16)
+#pragma unroll
+      for (int j = 0; j < QB; ++j) p1[j][0] = p1[j][1] = u32x4{0, 0, 0, 0};
+      uint32_t vat = at_stage(stage) + (uint32_t)(8 * (t % 2));      // (zeros times V of this page, which every row sees)
+      float vsb = lane_f(pvs, i - base);
       // A half step at t, then whether the segment ends. Where it has ended already (behind the
       // first of a pair: the loop has one exit, or the outputs would be copied at it), it is
       // no step: the product with pp and no probabilities.
@@ -900,11 +911,11 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
       } while (!done);
       product_v(vat, vsb, p1);
     }
-    for (int i = whole; i < last; ++i) {
-      sync(i);
+    for (int i = t / 2, half = t % 2; i < last; ++i, half = 0) {
+      if (synced != i) sync(i);
       const uint32_t at = at_stage(stage);
       stage = after(stage);
-      if (!none(i) && i * kPage < lim_w) masked_page(i, at, lane_f(pks, i - base), lane_f(pvs, i - base));
+      if (!none(i) && i * kPage < lim_w) masked_page(i, half, at, lane_f(pks, i - base), lane_f(pvs, i - base));
     }
   }
   wait_vm<0>();                                    // no DMA into LDS that another workgroup may get

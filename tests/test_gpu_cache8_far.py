@@ -28,9 +28,10 @@ def f3c(torch):
     return m
 
 
-def _pool(torch, f3c, gen, lens, heads, hd, low, high):
-    """(cache, K values float64 [sample][head][token], V the same with columns). K: e4m3 codes of 1 to 15/8 with a scale of
-    2^low to 2^high a page, of both signs; V random; NaN behind the last token."""
+def _pool(torch, f3c, gen, lens, heads, hd, low, high, v_exp=0, gone=()):
+    """(cache, K values float64 [sample][head][token], V the same with columns, whether a token is there [sample][token]).
+    K: e4m3 codes of 1 to 15/8 with a scale of 2^low to 2^high a page, of both signs; V random, times 2^v_exp; NaN behind
+    the last token. gone: (sample, page) that is none."""
     rng = np.random.default_rng(hd + sum(lens))
     need = [-(-n // 64) for n in lens]
     order = torch.from_numpy(rng.permutation(sum(need))).cuda()
@@ -45,9 +46,9 @@ def _pool(torch, f3c, gen, lens, heads, hd, low, high):
     k = code[..., None].expand(-1, -1, -1, hd).contiguous()
     v = torch.randn(pages, heads, 64, hd, generator=gen, device="cuda").to(torch.float8_e4m3fn).view(torch.uint8)
     ks = (127 + rand(low, high + 1, pages, heads)).to(torch.uint8)
-    vs = torch.full((pages, heads), 127, dtype=torch.uint8, device="cuda")
+    vs = torch.full((pages, heads), 127 + v_exp, dtype=torch.uint8, device="cuda")
     f8 = lambda x: x.view(torch.float8_e4m3fn).double()  # noqa: E731
-    kval, vval = f8(code) * torch.exp2(ks.double() - 127)[..., None], f8(v)
+    kval, vval = f8(code) * torch.exp2(ks.double() - 127)[..., None], f8(v) * 2.0 ** v_exp
     keys = [kval[table[b, :n].long()].transpose(0, 1).reshape(heads, -1)[:, :lens[b]] for b, n in enumerate(need)]
     vals = [vval[table[b, :n].long()].transpose(0, 1).reshape(heads, -1, hd)[:, :lens[b]] for b, n in enumerate(need)]
     for b, n in enumerate(lens):
@@ -55,18 +56,23 @@ def _pool(torch, f3c, gen, lens, heads, hd, low, high):
             k[table[b, n // 64], :, n % 64:] = v[table[b, n // 64], :, n % 64:] = 0x7F
     vt = torch.empty(pages, heads, hd, 64, dtype=torch.uint8, device="cuda")
     vt[..., torch.from_numpy(cache8.SLOTS).cuda()] = v.transpose(2, 3)
-    return f3c.Cache8(k, vt, ks, vs, table), keys, vals
+    there = [torch.ones(n, dtype=torch.bool, device="cuda") for n in lens]
+    for b, page in gone:
+        table[b, page] = -1
+        there[b][64 * page:64 * page + 64] = False
+    return f3c.Cache8(k, vt, ks, vs, table), keys, vals, there
 
 
-def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, prescaled=False):
+def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, gone=()):
     """qs: a query's value is drawn from these, with a sign; every eighth query is zeros.
 
-    Tolerance: ties have one probability p, so that a row is p sum(v) / (n p). In float32 its n sums are off by at most
-    n 2^-24 mean|v| each; a sum of probabilities that are not the rounded ones of the product (16 rows a workgroup) is
-    that of p = 1, exact; joins of parts multiply by 2^0 or by what is below e^-40 (gaps of a sixteenth of a score of
-    2^10 or more); 1 / n and its product 2^-23; the rounding to bf16 2^-8. Zeros queries: p = 1 for all keys."""
+    Tolerance: other keys lie 2^-4 of a score of 2^12 or more below, e^-100 at most. Equal keys have one probability, but
+    for its rounding to bf16 in the product with V, by 2^-8 at most, where the reference moves between them (to a sum's
+    logarithm): p(1 + d) in place of p turns a mean o of v into one off by the mean of d (v - o), 2^-8 (mean|v| + |o|) at
+    most. Exponentials, their references' and float32 sums of n terms: 2^-12 + n 2^-24 of mean|v|. Then o is rounded to
+    bf16, 2^-8."""
     gen = torch.Generator(device="cuda").manual_seed(hd * 7 + nq[0])
-    pool, keys, vals = _pool(torch, f3c, gen, lens, kv, hd, low, high)
+    pool, keys, vals, there = _pool(torch, f3c, gen, lens, kv, hd, low, high, v_exp, gone)
     off = [1]
     for n in nq:
         off.append(off[-1] + n)
@@ -79,17 +85,17 @@ def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, prescaled
     assert torch.equal(q.double().view(R, heads, hd)[..., 0], val)
     o = torch.full_like(q, 5.0)
     say("far scores", hd, kv, heads, nq, lens, causal, low, high, qs)
-    f3c.op_cache8_attention(pool, heads, off, lens, q, o, causal=causal, q_prescaled=prescaled)
+    f3c.op_cache8_attention(pool, heads, off, lens, q, o, causal=causal)
     torch.cuda.synchronize()
     assert bool((o[:1] == 5).all()) and bool((o[off[-1]:] == 5).all())
     for b, held in enumerate(lens):
         if not nq[b]:
             continue
         got = o[off[b]:off[b + 1]].double().view(nq[b], heads, hd)
-        see = torch.ones(nq[b], held, dtype=torch.bool, device="cuda")
+        see = there[b][None].expand(nq[b], held)
         if causal:
             last = held - nq[b] + torch.arange(nq[b], device="cuda")
-            see = torch.arange(held, device="cuda")[None] <= last[:, None]
+            see = see & (torch.arange(held, device="cuda")[None] <= last[:, None])
         for h in range(heads):
             g = h // (heads // kv)
             s = (val[off[b]:off[b + 1], h, None] * keys[b][g][None]).masked_fill(~see, float("-inf"))
@@ -97,7 +103,7 @@ def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, prescaled
             n = top.sum(1, keepdim=True).clamp(min=1)
             p = top.double() / n
             want, mag = p @ vals[b][g], p @ vals[b][g].abs()
-            tol = (n * 2.0 ** -24 + 2.0 ** -22) * mag + 1e-15 * vals[b][g].abs().max()
+            tol = (2.0 ** -8 + 2.0 ** -12 + n * 2.0 ** -24) * mag + 2.0 ** -8 * want.abs() + 1e-40 * vals[b][g].abs().max()
             tol = tol + 2.0 ** -8 * (want.abs() + tol)
             err = (got[:, h] - want).abs()
             assert bool((err <= tol).all()), (b, h, int((~(err <= tol)).any(1).nonzero()[0]), float(err.nan_to_num(9.0).max()))
@@ -113,3 +119,30 @@ def test_far_scores_in_one_masked_page(torch, f3c, hd, causal, low, high):
     """Fewer tokens than a page holds: 128 rows a workgroup (and 16)."""
     for kv, heads, nq, lens in ((8, 16, [2000], [63]), (2, 14, [1500, 1500], [41, 63]), (1, 1, [40], [50])):
         _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [8.0, 13.0, 120.0])
+
+
+# head width, K/V heads, heads, queries, tokens, causal: every form of the kernel that calls take (16, 128 and 256 rows a
+# workgroup, one and two groups of waves, pages whole and split), then rows enough for each form again under a mask
+FORMS = [(32, 1, 1, [37], [98], True), (32, 1, 1, [32], [3741], True), (32, 1, 4, [4017, 1340], [92, 47], False),
+         (32, 2, 8, [2528, 843], [1612, 807], False), (32, 2, 8, [2091, 698], [130, 66], False),
+         (32, 2, 8, [667, 223], [6761, 3381], True), (32, 8, 56, [616], [2385], False),
+         (32, 2, 14, [3254, 1085], [906, 454], False), (32, 1, 2, [2590, 864], [8147, 4074], False),
+         (64, 1, 1, [34], [94], True), (64, 1, 1, [34], [2292], False), (64, 4, 4, [3022, 1008], [91, 46], False),
+         (64, 1, 4, [2140], [4746], True), (64, 4, 28, [713], [389], False), (64, 1, 7, [445, 149], [5003, 2502], False),
+         (64, 8, 32, [3350], [129], False), (64, 8, 32, [783, 262], [3072, 1537], False),
+         (64, 8, 32, [1522, 508], [260, 131], False), (64, 4, 28, [882, 295], [1104, 553], False),
+         (128, 1, 1, [32], [104], False), (128, 1, 1, [40], [1273], True), (128, 8, 16, [608, 203], [90, 46], False),
+         (128, 8, 56, [67, 23], [1875, 938], False), (128, 2, 8, [1327, 443], [582, 292], False),
+         (128, 4, 4, [1032], [2379], False),
+         (32, 2, 14, [3254, 1085], [906, 454], True), (64, 4, 28, [882, 295], [1104, 553], True),
+         (128, 2, 8, [1327, 443], [582, 292], True)]
+
+
+@pytest.mark.parametrize("low,high", FAR + [(90, 99)])
+@pytest.mark.parametrize("hd,kv,heads,nq,lens,causal", FORMS)
+def test_far_scores_in_whole_pages(torch, f3c, hd, kv, heads, nq, lens, causal, low, high):
+    """References that begin far out, and (exponents of 10 to 40) that get there from page to page; values up to 2^99."""
+    _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [8.0, 13.0, 120.0])
+    pages = -(-lens[0] // 64)
+    gone = [(0, p) for p in {0, pages // 2, pages - 1}]
+    _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [1.0, 96.0], 97 if low == 10 else 0, gone)
