@@ -743,17 +743,14 @@ def _cache8(cache, batch: int, dev: int, T):
 
 def _ints(values):
     """Host integers of a call as a C array, made at each call (they change from token to token)."""
-    try:
-        return array("i", values)
-    except TypeError:                              # elements that are no integers by type
-        return array("i", [int(v) for v in values])
+    return array("i", values)
 
 
 def _samples(off, lens, rows: int):
     """(row offsets, samples, tokens held), as arrays; the library looks at their order."""
     try:
         offsets, held = _ints(off), _ints(lens)
-    except OverflowError:
+    except (OverflowError, TypeError):             # (an element that is no integer by type: 63.9 is no token count)
         raise ValueError("off, lens: 32-bit integers expected") from None
     B = len(held)
     if B < 1 or len(offsets) != B + 1 or offsets[0] < 0 or offsets[B] > rows:
