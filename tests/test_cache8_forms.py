@@ -11,7 +11,7 @@ import pytest
 
 from paper_2511_22533_amd import build, f3c
 from test_gpu_cache8 import ROWS
-from test_gpu_cache8_far import FORMS
+from test_gpu_cache8_far import DEEP, FORMS
 from test_gpu_cache8_long import LONG
 
 with open(os.path.join(build.CSRC, "k_cache8.hip")) as _f:
@@ -112,6 +112,12 @@ REACHED = {(hd, rows, groups, split) for hd in (32, 64, 128) for rows, groups in
 
 def test_calls_far_out_reach_every_form():
     assert {(c[0],) + form(*c)[:3] for c in FORMS} == REACHED
+
+
+def test_deep_calls_look_pages_up_twice():
+    forms = [form(*c, ws=0) for c in DEEP]
+    assert all(-(-c[4][0] // 64) > 64 * f[1] for c, f in zip(DEEP, forms))
+    assert {(c[0],) + f[:2] for c, f in zip(DEEP, forms)} == {r[:3] for r in REACHED if r[1] > 16} - {(32, 256, 1)}
 
 
 def test_calls_of_many_rows_reach_every_form_of_theirs():

@@ -63,7 +63,7 @@ def _pool(torch, f3c, gen, lens, heads, hd, low, high, v_exp=0, gone=()):
     return f3c.Cache8(k, vt, ks, vs, table), keys, vals, there
 
 
-def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, gone=()):
+def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, gone=(), workspace=None):
     """qs: a query's value is drawn from these, with a sign; every eighth query is zeros.
 
     Tolerance: other keys lie 2^-4 of a score of 2^12 or more below, e^-100 at most. Equal keys have one probability, but
@@ -85,7 +85,7 @@ def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, 
     assert torch.equal(q.double().view(R, heads, hd)[..., 0], val)
     o = torch.full_like(q, 5.0)
     say("far scores", hd, kv, heads, nq, lens, causal, low, high, qs)
-    f3c.op_cache8_attention(pool, heads, off, lens, q, o, causal=causal)
+    f3c.op_cache8_attention(pool, heads, off, lens, q, o, causal=causal, workspace=workspace)
     torch.cuda.synchronize()
     assert bool((o[:1] == 5).all()) and bool((o[off[-1]:] == 5).all())
     for b, held in enumerate(lens):
@@ -146,3 +146,18 @@ def test_far_scores_in_whole_pages(torch, f3c, hd, kv, heads, nq, lens, causal, 
     pages = -(-lens[0] // 64)
     gone = [(0, p) for p in {0, pages // 2, pages - 1}]
     _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [1.0, 96.0], 97 if low == 10 else 0, gone)
+
+
+# calls in one piece of more than 64 pages, which are looked up 64 at a time
+DEEP = [(32, 8, 32, [2055], [4419], False), (32, 8, 56, [456], [8462], True), (32, 8, 16, [2101], [8461], False),
+        (64, 8, 56, [1217], [4407], True), (64, 8, 56, [300], [8584], False), (64, 8, 32, [3138], [4668], False),
+        (64, 2, 14, [2395], [8439], True), (128, 8, 32, [1037], [4423], False), (128, 4, 28, [344], [8412], True)]
+
+
+@pytest.mark.parametrize("low,high", FAR)
+@pytest.mark.parametrize("hd,kv,heads,nq,lens,causal", DEEP)
+def test_far_scores_over_many_pages(torch, f3c, hd, kv, heads, nq, lens, causal, low, high):
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [8.0, 13.0, 120.0], workspace=none)
+    _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [1.0, 96.0], gone=[(0, 63), (0, 64), (0, 66)],
+           workspace=none)
