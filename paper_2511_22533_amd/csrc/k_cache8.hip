@@ -622,6 +622,8 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
   auto lane_f = [](float v, int i) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
   };
+  // (s_nop: the load's base, a scalar write of M0, wants one wait state, which the compiler does not place before
+  // inline assembly)
   auto fetch = [&](int i, int stage) {             // page i (of those looked up)
     const int page = __builtin_amdgcn_readlane(pg, i - base);
     const int64_t at = ((int64_t)page * kvh + head) * TILE;
@@ -631,7 +633,8 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
       const uint8_t* from = page < 0 ? reinterpret_cast<const uint8_t*>(kNoPage)
                                      : (blk < DMA ? p.c.k : p.c.v) + at + of * 1024;
       const uint32_t to = lds0 + (uint32_t)(stage * 2 * TILE + blk * 1024);
-      asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(blk < DMA ? kdma : vdma), "s"(from), "{m0}"(to) : "memory");
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                   : : "v"(blk < DMA ? kdma : vdma), "s"(from), "{m0}"(to) : "memory");
     }
   };
   // The reference of block j moves to `to`: what was summed up is scaled.

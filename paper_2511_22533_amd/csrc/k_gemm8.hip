@@ -412,27 +412,28 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) 
       for (int x = wave; x < blocks; x += NW) {
         const uint32_t at = (uint32_t)(64 * x + lane) * 4u, dst = lds0 + (uint32_t)(LDSB + first * 4 + x * 256);
         if (BM >= 64 || f || lane < BM)
-          asm volatile("buffer_load_dword %0, %1, 0 offen lds" : : "v"(at), "s"(d), "{m0}"(dst) : "memory");
+          asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" : : "v"(at), "s"(d), "{m0}"(dst) : "memory");
       }
     }
   }
-  // DMA instruction q of K tile t (t < KT)
+  // DMA instruction q of K tile t (t < KT). (s_nop: the load's base, a scalar write of M0, wants one wait
+  // state, which the compiler does not place before inline assembly.)
   auto fetch1 = [&](int q, int t, int stage) {
     const uint32_t k = (uint32_t)t * KTB;
     if (q < DQ) {
       const uint32_t dst = lds0 + (uint32_t)(stage * SBUF + (wave + NW * q) * 1024);
       if (q < DA / NW) {
-        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+        asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                      : : "v"(dofs[q]), "s"(adesc), "s"(k), "{m0}"(dst) : "memory");
       } else {
-        asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+        asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                      : : "v"(dofs[q]), "s"(wdesc), "s"(k), "{m0}"(dst) : "memory");
       }
     } else {
       const int y = q - DQ;
       const uint32_t dst = lds0 + (uint32_t)(STAGES * SBUF + stage * SSET + (wave + NW * y) * 256);
       const uint32_t ks = (uint32_t)(t & ~3);
-      asm volatile("buffer_load_dword %0, %1, %2 offen lds"
+      asm volatile("s_nop 0\n\tbuffer_load_dword %0, %1, %2 offen lds"
                    : : "v"(sofs[y]), "s"(sdesc[y]), "s"(ks), "{m0}"(dst) : "memory");
     }
   };
