@@ -139,10 +139,12 @@ __device__ __forceinline__ int xcd_logical_id(int hw, int total) {
 // kind before any LDS read. A kernel using it orders these loads itself (an
 // s_waitcnt on the vector-memory counter and a barrier before a tile is
 // read); waits the compiler places for its own loads only grow more
-// conservative, since the counter retires in issue order.
+// conservative, since the counter retires in issue order. The load wants one wait
+// state behind a scalar write of M0, which the compiler does not place before
+// inline assembly.
 __device__ __forceinline__ void dma16(const char* gptr, char* lds_block) {
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_block;
-  asm volatile("global_load_lds_dwordx4 %0, off" : : "v"(gptr), "{m0}"(__builtin_amdgcn_readfirstlane(base))
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gptr), "{m0}"(__builtin_amdgcn_readfirstlane(base))
                : "memory");
 }
 

@@ -284,6 +284,7 @@ __global__ __launch_bounds__(64 * NW, QB) void k_attn(AttnArgs p) {
     vofs[q] = row * ldv_b + (uint32_t)((phys ^ (((row >> 1) & 1) << 2)) << 4);
     asm("" : "+v"(kofs[q]), "+v"(vofs[q]));            // kept, not recomputed per tile
   }
+  // (s_nop: the wait state between a scalar write of M0 and a load that takes its base from it)
   auto fetch_dma = [&](int kv0, int stage, int k) {
 #pragma unroll
     for (int q = 0; q < DQ; ++q) {
@@ -291,8 +292,8 @@ __global__ __launch_bounds__(64 * NW, QB) void k_attn(AttnArgs p) {
       const uint32_t ko = kofs[q] + (uint32_t)kv0 * ldk_b, vo = vofs[q] + (uint32_t)kv0 * ldv_b;
       const uint32_t kl = lds_u + (uint32_t)((stage * KS + k) * KBUF + blk_u * 1024);
       const uint32_t vl = lds_u + (uint32_t)(VREG + (stage * KS + k) * VBUF + blk_u * 1024);
-      asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(ko), "s"(kdesc), "{m0}"(kl) : "memory");
-      asm volatile("buffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(vo), "s"(vdesc), "{m0}"(vl) : "memory");
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(ko), "s"(kdesc), "{m0}"(kl) : "memory");
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(vo), "s"(vdesc), "{m0}"(vl) : "memory");
     }
   };
 

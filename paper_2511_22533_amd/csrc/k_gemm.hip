@@ -289,16 +289,16 @@ __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm_dma(GemmArgs p) {
     asm("" : "+v"(dofs[q]));
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  // DMA instruction q of K tile kt
+  // DMA instruction q of K tile kt (s_nop: the wait state behind a scalar write of M0)
   auto fetch1 = [&](int q, uint32_t k, int stage) {
     const uint32_t dst = lds0 + (uint32_t)(stage * SBUF + (wave + NW * q) * 1024);
     if constexpr (WIDE) {
       dma16(dsrc[q] + k, lds + stage * SBUF + (wave + NW * q) * 1024);
     } else if (q < DA / NW) {
-      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                    : : "v"(dofs[q]), "s"(adesc), "s"(k), "{m0}"(dst) : "memory");
     } else {
-      asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds"
+      asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                    : : "v"(dofs[q]), "s"(wdesc), "s"(k), "{m0}"(dst) : "memory");
     }
   };
