@@ -465,13 +465,16 @@ int f3c_op_gemm_i8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void
  * may change between calls); samples may share pages that are no longer written. An
  * entry outside [0, n_pages) is no page: nothing is written to it, and attention passes
  * its tokens over. All pointers are device memory, k and v 16-byte aligned, table
- * 4-byte. The tiles' bytes behind a sample's last token are neither written nor used. */
+ * 4-byte. The tiles' bytes behind a sample's last token are neither written nor used.
+ * Lengths and offsets are host values that a call reads before it returns: a captured
+ * graph keeps those of its capture (and reads pages, table and rows at each replay), so a
+ * step whose lengths grow is captured anew for each length. At most F3C_MAX_BATCH samples. */
 #define F3C_PAGE_TOKENS 64
 typedef struct {
   int32_t kv_heads;         /* 1..1024 */
   int32_t head_dim;         /* 32, 64 or 128 */
   int32_t n_pages;          /* of the pool */
-  int32_t max_pages;        /* entries of a sample's row of table */
+  int32_t max_pages;        /* entries of a sample's row of table, at most 2^24 */
   void* k;                  /* e4m3 [n_pages][kv_heads][64 * head_dim] */
   void* v;
   void* k_scale;            /* E8M0 [n_pages][kv_heads] */
@@ -495,18 +498,22 @@ int f3c_op_cache8_append(const f3c_cache8* cache, int32_t dtype, int32_t batch, 
 
 /* Attention over it, f3c_op_attention's on bf16 rows: queries q_off[b]..q_off[b+1] of q
  * [.][ldq] and their outputs o [.][ldo] (heads * head_dim columns; query head h reads key
- * head h / (heads / kv_heads)) over the len[b] tokens of sample b; o = softmax(q K^T /
- * sqrt(head_dim)) V. causal: a sample's queries are its last tokens, query i of n seeing
- * tokens 0..len - n + i. A query that sees no token gets zeros. q_prescaled as in
+ * head h / (heads / kv_heads)) over the len[b] tokens of sample b, at most 64 * max_pages;
+ * o = softmax(q K^T / sqrt(head_dim)) V, probabilities rounded to bf16 for the product
+ * with V. causal: a sample's queries are its last tokens, query i of n seeing tokens
+ * 0..len - n + i. A query that sees no token gets zeros. q_prescaled as in
  * f3c_op_attention. Any finite scores; tiles' values between 2^-100 and 2^100 in
  * magnitude (a token whose share is below 2^-102 of the row's largest may count as none).
  * NaN in a token reaches the queries that see it and no others. workspace
  * (device, 16-byte aligned, may be NULL): the key range is split over workgroups where
  * there are few queries, as far as the workspace holds the splits' results;
  * f3c_op_cache8_attention_bytes says how much the call makes use of (it looks at no device
- * memory: pointers may be NULL). Rows of q 16-byte aligned, of o 8-byte. ceil(queries * heads /
- * kv_heads / 16) * kv_heads summed over samples below 2^22; heads at most 65535.
- * Errors: F3C_EINVAL. */
+ * memory: pointers may be NULL). Calls that may run at once, graphs among them, need
+ * workspaces of their own. The same call gives the same bits. A query's roundings follow
+ * the kernel's form and splits, which the sizes of all samples and of the workspace choose,
+ * and in calls of many queries those beside it, whose references move together.
+ * Rows of q 16-byte aligned, of o 8-byte. ceil(queries * heads / kv_heads / 16) * kv_heads
+ * summed over samples below 2^22; heads at most 65535. Errors: F3C_EINVAL. */
 int f3c_op_cache8_attention_bytes(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,
                                   const int32_t* len_host, int32_t causal, size_t* bytes);
 int f3c_op_cache8_attention(const f3c_cache8* cache, int32_t heads, int32_t batch, const int32_t* q_off_host,

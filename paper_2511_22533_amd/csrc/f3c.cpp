@@ -1165,8 +1165,8 @@ int f3c_op_gemm_i8(int32_t epilogue, int32_t M, int32_t N, int32_t K, const void
   return F3C_OK;
 }
 
-// A cache's sizes, the samples' rows and the tokens that their pages hold (up to `extra`
-// more with a sample's rows).
+// A cache's sizes, the samples' rows and the tokens that their pages hold; append: the rows
+// become tokens behind those, and have to fit beside them.
 static int check_cache8(const f3c_cache8* cache, int32_t batch, const int32_t* off_host, const int32_t* len_host,
                         bool append, Cache8* c, Segs* rows, Lens* len) {
   if (!cache || !off_host || !len_host) return fail(F3C_EINVAL, "NULL argument");

@@ -760,7 +760,7 @@ def _samples(off, lens, rows: int):
 
 def op_cache8_append(dtype: int, cache, lens: Sequence[int], off: Sequence[int], k, v, stream=None):
     """Rows off[b]..off[b+1] of k and v [R][heads * head_dim] become tokens lens[b].. of sample b (cache: a Cache8, or its
-    five tensors)."""
+    five tensors). lens and off are integers of the host: a captured graph keeps their values."""
     T = _dtypes()
     if dtype not in (F3C_F32, F3C_BF16) or k.dim() != 2:
         raise ValueError("rows of dtype F3C_F32 or F3C_BF16 expected")
@@ -776,7 +776,8 @@ def op_cache8_append(dtype: int, cache, lens: Sequence[int], off: Sequence[int],
 def op_cache8_attention(cache, heads: int, q_off: Sequence[int], lens: Sequence[int], q, o, causal: bool = False,
                         q_prescaled: bool = False, workspace=None, stream=None):
     """Attention of bf16 queries q [R][heads * head_dim] over the lens[b] tokens that the cache holds of each sample,
-    into o. workspace: a device tensor that the call may use, as large as it is (allocated here if None)."""
+    into o. workspace: a device tensor that the call may use, as large as it is (allocated here if None); calls that may
+    run at once need their own. q_off and lens are integers of the host: a captured graph keeps their values."""
     T = _dtypes()
     torch = T["torch"]
     if q.dim() != 2:
