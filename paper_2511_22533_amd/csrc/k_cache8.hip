@@ -503,9 +503,9 @@ __device__ const u32x4 kNoPage[64] = {};
 // with two), many tiles one, whose workgroups hide each other's beginnings and ends (4096
 // over 4096: 145 against 149).
 //
-// Bound by vector issue: at 9831 queries over 32768 tokens, 16 heads of 64 (1388 us, 950 TFLOP/s),
+// Bound by vector issue: at 9831 queries over 32768 tokens, 16 heads of 64 (1371 us, 962 TFLOP/s),
 // it is busy 63% of the cycles (exponentials and roundings to bf16 half of that, widening a
-// quarter), the matrix pipes 46%; over 1374 tokens (32768 queries, 213 us, 865 TFLOP/s) the first
+// quarter), the matrix pipes 46%; over 1374 tokens (32768 queries, 211 us, 873 TFLOP/s) the first
 // and the last of 22 pages show. 64 rows a wave (QB 2) share each widening: 1744 us with 32 there.
 template <int HD, int QB, int NW, int NG>
 __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {

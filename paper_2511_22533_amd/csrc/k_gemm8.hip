@@ -22,8 +22,8 @@
 // in any order. The tiles are chosen by e4m3's table: over 1200 calls of integers (1 to 32768
 // rows, 128 to 8192 columns and K) its pick is 0.5% from the best of the nine in the mean, 16% at worst;
 // a table fitted to those calls 0.6%. 8192 x 8192 x 8192 runs at 2160 to 2260 TOP/s on random bytes,
-// 32768 x 4096 x 1024 with GELU in 175 to 196 us by card: power, and matrix pipes 41%, vector
-// issue 56% of the cycles.
+// 32768 x 4096 x 1024 with GELU in 175 to 196 us by card: matrix pipes 41% of the cycles and vector
+// issue 56%, products and epilogues in turn, at a clock of 1.85 GHz.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -324,7 +324,7 @@ __device__ __forceinline__ void gemm8_epilogue(const Gemm8Args& p, Acc<OPS> (&ac
 // Against the bf16 projections on one card (us, bf16 / here): 32768 x 4096 x 1024 GELU
 // 300 / 161 (out in 8 bits), 9831 x 2048 x 1024 55 / 29, 9831 x 1024 x 1024 gated residual 35 / 26;
 // on exact products, gated residual: 32768 x 1024 x 4096 271 / 232, 9831 rows 91 / 86, 820 rows
-// 18.6 / 18.7.
+// 18.6 / 19.2.
 template <int BM, int BN, int WGM, int WGN, int STAGES, int OCC, int EPI, int DPI = 1, int OPS = OPS_FP8>
 __global__ __launch_bounds__(64 * WGM * WGN, OCC) void k_gemm8_dma(Gemm8Args p) {
   constexpr int NW = WGM * WGN, WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 32, TN = WTN / 32;
