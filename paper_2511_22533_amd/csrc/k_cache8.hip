@@ -566,10 +566,12 @@ __global__ __launch_bounds__(64 * NW * NG, 2) void k_cache8_rows(Attn8Args p) {
   // leave outputs of values up to 2^100 within range. What is below 2^-102 of a row's largest
   // probability may count as none: exponentials end at 2^-126.)
   // Whole pages take their exponents by one fma, which rounds s c - m once, where m is a
-  // rounded s c: the largest key's is half a step of m off 0. Up to kNear that is 2^-1 at most, so
-  // that a step behind a moved reference adds less than 2^14 and is kept; rows further out
-  // (finite: infinite scores are NaN in any way) take their pages one step after the other.
-  constexpr float kMost = 0x1p24f, kNear = 0x1p23f;
+  // rounded s c: the largest key's is half a last place of m off 0. Up to kNear that is 2^-13 at
+  // most: nothing beside keys of the same score in pages that round s c first, as those with
+  // masks do, and a step behind a moved reference adds less than 2^13 to a sum and is kept.
+  // Rows further out (finite: infinite scores are NaN in any way) take their pages one step after
+  // the other.
+  constexpr float kMost = 0x1p24f, kNear = 0x1p12f;
   f32x16 o[QB][NV];
   float m[QB];
   f32x4 l[QB];

@@ -2,8 +2,8 @@
 probability, whatever its size, and a call must end.
 
 A key's columns all hold one value and a query's too, so that every score is an exact float32 number: equal keys tie
-exactly, and other keys lie a sixteenth of the score below. A row's output is then the plain mean of V over the keys of
-its largest score; a query of zeros sees all its keys alike.
+exactly, and other keys lie a sixteenth of the score below. Where scores are large a row's output is the plain mean of V over
+the keys of its largest one; a query of zeros sees all its keys alike.
 """
 import numpy as np
 import pytest
@@ -28,9 +28,9 @@ def f3c(torch):
     return m
 
 
-def _pool(torch, f3c, gen, lens, heads, hd, low, high, v_exp=0, gone=()):
+def _pool(torch, f3c, gen, lens, heads, hd, low, high, v_exp=0, gone=(), signs=2):
     """(cache, K values float64 [sample][head][token], V the same with columns, whether a token is there [sample][token]).
-    K: e4m3 codes of 1 to 15/8 with a scale of 2^low to 2^high a page, of both signs; V random, times 2^v_exp; NaN behind
+    K: e4m3 codes of 1 to 15/8 with a scale of 2^low to 2^high a page, of both signs (or signs 1); V random, times 2^v_exp; NaN behind
     the last token. gone: (sample, page) that is none."""
     rng = np.random.default_rng(hd + sum(lens))
     need = [-(-n // 64) for n in lens]
@@ -42,7 +42,7 @@ def _pool(torch, f3c, gen, lens, heads, hd, low, high, v_exp=0, gone=()):
         table[b, :n] = order[at:at + n].int()
         at += n
     rand = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=gen, device="cuda")  # noqa: E731
-    code = (0x38 + rand(0, 8, pages, heads, 64) + 0x80 * rand(0, 2, pages, heads, 64)).to(torch.uint8)
+    code = (0x38 + rand(0, 8, pages, heads, 64) + 0x80 * rand(0, signs, pages, heads, 64)).to(torch.uint8)
     k = code[..., None].expand(-1, -1, -1, hd).contiguous()
     v = torch.randn(pages, heads, 64, hd, generator=gen, device="cuda").to(torch.float8_e4m3fn).view(torch.uint8)
     ks = (127 + rand(low, high + 1, pages, heads)).to(torch.uint8)
@@ -63,16 +63,18 @@ def _pool(torch, f3c, gen, lens, heads, hd, low, high, v_exp=0, gone=()):
     return f3c.Cache8(k, vt, ks, vs, table), keys, vals, there
 
 
-def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, gone=(), workspace=None):
+def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, gone=(), workspace=None, signs=2):
     """qs: a query's value is drawn from these, with a sign; every eighth query is zeros.
 
-    Tolerance: other keys lie 2^-4 of a score of 2^12 or more below, e^-100 at most. Equal keys have one probability, but
-    for its rounding to bf16 in the product with V, by 2^-8 at most, where the reference moves between them (to a sum's
-    logarithm): p(1 + d) in place of p turns a mean o of v into one off by the mean of d (v - o), 2^-8 (mean|v| + |o|) at
-    most. Exponentials, their references' and float32 sums of n terms: 2^-12 + n 2^-24 of mean|v|. Then o is rounded to
-    bf16, 2^-8."""
+    Tolerance: scores are exact but for their scale, 3 roundings of 2^-24; other keys lie 2^-4 of the score below, so that
+    they count (above e^-30) where it is below 480 alone: e^ds is 1 within 2^-13.4 there. Probabilities are rounded to bf16
+    in the product with V, by 2^-8 at most: p(1 + d) in place of p, in the product alone or in the sum too, puts a mean o
+    of v off by 2^-8 (mean|v| + |o|) at most (equal keys as well, where the reference moves between them). Those scores,
+    exponentials, their references' moves: 2^-12 of mean|v|; float32 sums of n terms: n 2^-24. A key below 2^-102 of the
+    largest may count as none (exponentials end at 2^-126, taken against a reference within 2^24 of the largest): n of
+    them lose n 2^-102 max|v|. Then o is rounded to bf16, 2^-8."""
     gen = torch.Generator(device="cuda").manual_seed(hd * 7 + nq[0])
-    pool, keys, vals, there = _pool(torch, f3c, gen, lens, kv, hd, low, high, v_exp, gone)
+    pool, keys, vals, there = _pool(torch, f3c, gen, lens, kv, hd, low, high, v_exp, gone, signs)
     off = [1]
     for n in nq:
         off.append(off[-1] + n)
@@ -98,12 +100,12 @@ def _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, qs, v_exp=0, 
             see = see & (torch.arange(held, device="cuda")[None] <= last[:, None])
         for h in range(heads):
             g = h // (heads // kv)
-            s = (val[off[b]:off[b + 1], h, None] * keys[b][g][None]).masked_fill(~see, float("-inf"))
-            top = (s == s.amax(1, keepdim=True)) & see
-            n = top.sum(1, keepdim=True).clamp(min=1)
-            p = top.double() / n
+            s = (val[off[b]:off[b + 1], h, None] * keys[b][g][None] * hd ** 0.5).masked_fill(~see, float("-inf"))
+            n = see.sum(1, keepdim=True)
+            p = torch.softmax(s, 1).nan_to_num(nan=0.0)
             want, mag = p @ vals[b][g], p @ vals[b][g].abs()
-            tol = (2.0 ** -8 + 2.0 ** -12 + n * 2.0 ** -24) * mag + 2.0 ** -8 * want.abs() + 1e-40 * vals[b][g].abs().max()
+            tol = (2.0 ** -8 + 2.0 ** -12 + n * 2.0 ** -24) * mag + 2.0 ** -8 * want.abs()
+            tol = tol + n * 2.0 ** -102 * vals[b][g].abs().max()
             tol = tol + 2.0 ** -8 * (want.abs() + tol)
             err = (got[:, h] - want).abs()
             assert bool((err <= tol).all()), (b, h, int((~(err <= tol)).any(1).nonzero()[0]), float(err.nan_to_num(9.0).max()))
@@ -161,3 +163,14 @@ def test_far_scores_over_many_pages(torch, f3c, hd, kv, heads, nq, lens, causal,
     _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [8.0, 13.0, 120.0], workspace=none)
     _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [1.0, 96.0], gone=[(0, 63), (0, 64), (0, 66)],
            workspace=none)
+
+
+@pytest.mark.parametrize("hd,kv,heads,nq,lens,causal", FORMS + DEEP)
+def test_far_scores_of_one_sign(torch, f3c, hd, kv, heads, nq, lens, causal):
+    """Keys of one sign: half of the queries see negative scores alone, whose references come nearer from page to page, and
+    references on both sides of those that whole pages keep to (2^12)."""
+    for low, high in ((10, 40), (14, 18), (-6, 6), (0, 20)):
+        _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [8.0, 13.0, 120.0], signs=1)
+    for low, high in ((14, 18), (0, 20)):
+        _check(torch, f3c, hd, kv, heads, nq, lens, causal, low, high, [8.0, 13.0, 120.0],
+               workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
