@@ -131,7 +131,7 @@ FORMS = [(32, 1, 1, [37], [98], True), (32, 1, 1, [32], [3741], True), (32, 1, 4
          (32, 2, 14, [3254, 1085], [906, 454], False), (32, 1, 2, [2590, 864], [8147, 4074], False),
          (64, 1, 1, [34], [94], True), (64, 1, 1, [34], [2292], False), (64, 4, 4, [3022, 1008], [91, 46], False),
          (64, 1, 4, [2140], [4746], True), (64, 4, 28, [713], [389], False), (64, 1, 7, [445, 149], [5003, 2502], False),
-         (64, 8, 32, [3350], [129], False), (64, 8, 32, [783, 262], [3061, 1530], False),
+         (64, 8, 32, [3350], [129], False), (64, 8, 32, [783, 262], [3050, 1540], False),
          (64, 8, 32, [1522, 508], [260, 131], False), (64, 4, 28, [882, 295], [1104, 553], False),
          (128, 1, 1, [32], [104], False), (128, 1, 1, [40], [1273], True), (128, 8, 16, [608, 203], [90, 46], False),
          (128, 8, 56, [67, 23], [1875, 938], False), (128, 2, 8, [1327, 443], [582, 292], False),
